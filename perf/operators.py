@@ -220,7 +220,8 @@ def _dequantised(q, scale):
 def _to_e4m3(blocks, most):
     """Values of blocks scaled so that `most`, their largest magnitude, becomes 448, and the scales."""
     most = most.clamp_min(FLOOR)
-    return (blocks * (E4M3_MAX / most)).to(torch.float8_e4m3fn), most / E4M3_MAX
+    # (a number over a tensor would be its rounded reciprocal times the number)
+    return (blocks * (torch.full_like(most, E4M3_MAX) / most)).to(torch.float8_e4m3fn), most / E4M3_MAX
 
 
 def _padded(x, rows, cols):
