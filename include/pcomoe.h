@@ -90,7 +90,8 @@ typedef enum pcm_op {
     PCM_OP_ROUTE_SCORED = 4,
     PCM_OP_LAYER_PER_PATH = 5,
     PCM_OP_ROUTE_LOGITS = 6,
-    PCM_OP_ROUTE_PATHS = 7
+    PCM_OP_ROUTE_PATHS = 7,
+    PCM_OP_GROUPED_DX = 8
 } pcm_op;
 
 /* Path table and grouped dispatch layout of T tokens (caller-owned device buffers).
@@ -308,6 +309,78 @@ pcm_status pcm_project_combine_scored(pcm_dtype dtype, const void* u, const void
                                       const pcm_scored_paths* paths, int64_t T, int H, int F,
                                       int n, int K, float* y, int accumulate, void* ws,
                                       size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------- experts' products on their own
+ * The matrix products of the layer without what is fused around them, with their gradients, and in
+ * 8-bit floating point: for training, and for experts whose weights are held in 8 bits.
+ *
+ * Rows and groups are those of the path tables: row r belongs to group e where
+ * offsets[e] <= r < offsets[e+1] (offsets [n+1] i32, ascending from offsets[0] >= 0; empty groups are
+ * allowed), and comes from row s(r) = row_token[r] of x, or r where row_token is NULL (then T = R).
+ * offsets = NULL: one group (n = 1) of all R rows, row_token NULL: a plain product. R counts the rows of
+ * the row buffers: rows from offsets[n] on are neither read nor written. Offsets are held inside [0, R]
+ * and gathered indices inside [0, T), so no value of theirs reaches outside the buffers.
+ * Limits: K and N multiples of 16; n <= 256; R and T below 2^30. Sums are float32. Deterministic. */
+
+/* y[r, :] = x[s(r), :] W[e]^T for the rows r of group e. x [T,K] and w [n,N,K] of `dtype` (PCM_F32 or
+ * PCM_BF16), y [R,N] of out_dtype: PCM_F32, or for bf16 operands also PCM_BF16 (each float32 sum rounded
+ * once, to nearest even). */
+pcm_status pcm_grouped_gemm(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const void* w,
+                            const int32_t* offsets, const int32_t* row_token, int64_t T, int64_t R,
+                            int K, int N, int n, void* y, void* stream);
+
+/* Gradient by x of pcm_grouped_gemm. dy [R,N] and w [n,N,K] of `dtype`. row_of = NULL: dx [R,K],
+ * dx[r, :] = dy[r, :] W[e] (T = R, k = 1). row_of [T,k] i32 (the rows that read each row of x, as in
+ * pcm_paths; negative: none): dx [T,K], the sum of those rows' gradients, slots ascending, in float32,
+ * rounded once; every row of dx is written. k is at most 8 and R at most T*k.
+ * ws: pcm_workspace_bytes(PCM_OP_GROUPED_DX, T, K, 0, n, k, dtype) bytes where row_of is given. */
+pcm_status pcm_grouped_gemm_dx(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* w,
+                               const int32_t* offsets, const int32_t* row_of, int64_t T, int k,
+                               int64_t R, int K, int N, int n, void* dx, void* ws, size_t ws_bytes,
+                               void* stream);
+
+/* Gradient by w of pcm_grouped_gemm: dw[e] = [dw[e] +] sum over the rows r of group e of
+ * dy[r, :]^T x[s(r), :]. x [T,K], dy [R,N] of `dtype`, dw [n,N,K] of out_dtype. accumulate adds into dw
+ * (PCM_F32 only: a sum over calls is held in 32 bits); otherwise an empty group's dw is zero. */
+pcm_status pcm_grouped_gemm_dw(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const void* dy,
+                               const int32_t* offsets, const int32_t* row_token, int64_t T, int64_t R,
+                               int K, int N, int n, void* dw, int accumulate, void* stream);
+
+/* 8-bit values (OCP e4m3: sign, 4 exponent bits, 3 mantissa bits, largest 448, NaN but no infinity) with
+ * a float32 scale for each block of 128: the value stands for code * scale. A block whose largest finite
+ * magnitude is m has a = max(m, 2^-100), scale = a / 448, code = e4m3(v * (448 / a)), all float32
+ * operations, the code to nearest even. Infinities and NaN become NaN codes and leave the scale alone.
+ *
+ * Rows, blocks of 128 along a row (the last one shorter where K is no multiple): x [R,K] of `dtype`,
+ * q [R,K] u8, scale [R, ceil(K/128)] f32. count: device pointer to the number of rows to do (such as
+ * offsets + n; rows from there on are left as they were), NULL: all R. */
+pcm_status pcm_quant_fp8_rows(pcm_dtype dtype, const void* x, const int32_t* count, int64_t R, int K,
+                              uint8_t* q, float* scale, void* stream);
+
+/* The same for SiLU(gate) * up (Section 4.1's expansion, float32 in between): gate_up [R, 2F], a row's
+ * gate values before its up values; q [R,F], scale [R, ceil(F/128)]. */
+pcm_status pcm_swiglu_quant_fp8(pcm_dtype dtype, const void* gate_up, const int32_t* count, int64_t R,
+                                int F, uint8_t* q, float* scale, void* stream);
+
+/* Weights in blocks of 128 x 128: w [n,N,K] of `dtype`, q [n,N,K] u8, scale [n, ceil(N/128),
+ * ceil(K/128)] f32. q_t [n,K,N] and scale_t [n, ceil(K/128), ceil(N/128)] (both or neither): the same
+ * codes and scales of every W^T, with which pcm_grouped_gemm_fp8 gives the gradient by its input. */
+pcm_status pcm_quant_fp8_weights(pcm_dtype dtype, const void* w, int n, int N, int K, uint8_t* q,
+                                 float* scale, uint8_t* q_t, float* scale_t, void* stream);
+
+/* pcm_grouped_gemm of 8-bit operands: y[r, c] = sum over the blocks b of K of
+ * x_scale[s(r), b] w_scale[e, c / 128, b] sum over k in b of x[s(r), k] w[e, c, k].
+ * x [T,K] u8 with x_scale [T, ceil(K/128)], w [n,N,K] u8 with w_scale [n, ceil(N/128), ceil(K/128)] (any
+ * float32 scales), y [R,N] of out_dtype. The scaled blocks are added in float32. PCM_F32: so are a block's
+ * products (as bf16 values, exactly, at half the rate). PCM_BF16: on the 8-bit matrix cores, which cut
+ * products below 2^-13 of the largest among their neighbours (1.3e-5 of the result's norm on normal
+ * values; the rounding to bf16 is 1.7e-3).
+ * Backward: the gradient by the input is this call with dy quantised by rows and W^T's codes; the weight
+ * gradient's sum runs over rows, along which these scales are not shared: pcm_grouped_gemm_dw. */
+pcm_status pcm_grouped_gemm_fp8(pcm_dtype out_dtype, const uint8_t* x, const float* x_scale,
+                                const uint8_t* w, const float* w_scale, const int32_t* offsets,
+                                const int32_t* row_token, int64_t T, int64_t R, int K, int N, int n,
+                                void* y, void* stream);
 
 /* ---------------------------------------------------------------- tests and measurement
  * A layer never needs these. The *_tuned calls are the calls above with a pcm_tuning that

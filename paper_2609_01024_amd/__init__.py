@@ -14,6 +14,8 @@ from .binding import (BETA_GLOBAL, BETA_PRODUCT, BETA_SRC_COND, PCM_BF16, PCM_BF
                       pcm_residual_add, pcm_route, pcm_route_logits, pcm_route_scored,
                       pcm_mask_pack, pcm_route_paths, pcm_widen_f16,
                       capture_graph, workspace_bytes)
+from .experts import (pcm_grouped_gemm, pcm_grouped_gemm_dw, pcm_grouped_gemm_dx, pcm_grouped_gemm_fp8,
+                      pcm_quant_fp8_rows, pcm_quant_fp8_weights, pcm_swiglu_quant_fp8)
 
 __all__ = ["BETA_GLOBAL", "BETA_PRODUCT", "BETA_SRC_COND", "PCM_BF16", "PCM_BF16_F16DOWN", "PCM_F32",
            "LayerPlan",
@@ -24,4 +26,6 @@ __all__ = ["BETA_GLOBAL", "BETA_PRODUCT", "BETA_SRC_COND", "PCM_BF16", "PCM_BF16
            "pcm_project_combine_scored",
            "pcm_residual_add", "pcm_route", "pcm_route_logits", "pcm_route_scored",
            "pcm_mask_pack", "pcm_route_paths", "pcm_widen_f16",
-           "capture_graph", "workspace_bytes"]
+           "capture_graph", "workspace_bytes",
+           "pcm_grouped_gemm", "pcm_grouped_gemm_dw", "pcm_grouped_gemm_dx", "pcm_grouped_gemm_fp8",
+           "pcm_quant_fp8_rows", "pcm_quant_fp8_weights", "pcm_swiglu_quant_fp8"]

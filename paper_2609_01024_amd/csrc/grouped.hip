@@ -1,0 +1,71 @@
+// Products grouped by expert with ragged row counts, and their gradients (bf16 and float32 operands,
+// float32 sums):
+//   forward          y[r, :]  = x[s(r), :] W[e]^T          W [n, N, K], rows r of group e
+//   input gradient   dx[r, :] = dy[r, :] W[e]              (then summed over the rows of a token)
+//   weight gradient  dW[e]    = sum_r dy[r, :]^T x[s(r), :]
+#include "grouped.h"
+
+namespace pcm {
+namespace {
+
+using Small = TileCfg<64, 64, 2, 2, 3>;
+
+template <class E, bool DX, class OUT>
+hipError_t rows_by_shape(const GroupArgs& g, hipStream_t s) {
+    return launch_rows<E, Small, DX, OUT>(g, 8, s);
+}
+
+template <bool DX>
+hipError_t rows_by_type(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s) {
+    if (!bf16) return rows_by_shape<TF32, DX, float>(g, s);
+    return out_bf16 ? rows_by_shape<TBf16, DX, __bf16>(g, s) : rows_by_shape<TBf16, DX, float>(g, s);
+}
+
+template <class E, class OUT, bool ADD>
+hipError_t outer_by_shape(const GroupArgs& g, hipStream_t s) {
+    return launch_outer<E, Small, OUT, ADD>(g, s);
+}
+
+// A thread adds four columns of a token's rows, slots ascending, in float32.
+template <class OUT>
+__global__ __launch_bounds__(256) void slot_sum_kernel(const float* __restrict__ rows, const int32_t* __restrict__ row_of,
+                                                       int64_t T, int k, int64_t R, int K, OUT* __restrict__ out) {
+    const int64_t per = K / 4, total = T * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / per, c = (i - t * per) * 4;
+        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int a = 0; a < k; ++a) {
+            const int64_t r = row_of[t * k + a];
+            if (r < 0 || R == 0) continue;
+            sum += *(const floatx4*)(rows + (r < R ? r : R - 1) * K + c);
+        }
+        store4(out + t * K + c, sum);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_grouped(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s) {
+    return rows_by_type<false>(bf16, out_bf16, g, s);
+}
+
+hipError_t launch_grouped_dx(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s) {
+    return rows_by_type<true>(bf16, out_bf16, g, s);
+}
+
+hipError_t launch_grouped_dw(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s) {
+    if (!bf16) return g.accumulate ? outer_by_shape<TF32, float, true>(g, s) : outer_by_shape<TF32, float, false>(g, s);
+    if (out_bf16) return outer_by_shape<TBf16, __bf16, false>(g, s);
+    return g.accumulate ? outer_by_shape<TBf16, float, true>(g, s) : outer_by_shape<TBf16, float, false>(g, s);
+}
+
+hipError_t launch_slot_sum(const float* rows, const int32_t* row_of, int64_t T, int k, int64_t R, int K, void* out,
+                           bool out_bf16, hipStream_t s) {
+    const int64_t blocks = ceil_div(T * (K / 4), 256);
+    const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)));
+    if (out_bf16) slot_sum_kernel<<<grid, dim3(256), 0, s>>>(rows, row_of, T, k, R, K, (__bf16*)out);
+    else slot_sum_kernel<<<grid, dim3(256), 0, s>>>(rows, row_of, T, k, R, K, (float*)out);
+    return hipGetLastError();
+}
+
+}  // namespace pcm

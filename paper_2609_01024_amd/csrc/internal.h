@@ -255,4 +255,35 @@ hipError_t launch_route_scored(const float* g_base, const float* g_tgt, float la
                                int32_t* n_src, int32_t* src_expert, int32_t* n_tgt,
                                int32_t* tgt_expert, uint64_t* bits, float* beta, hipStream_t s);
 
+// Products grouped by expert and their gradients (grouped.hip), and the 8-bit product (fp8.hip).
+struct GroupArgs {
+    const void* a;            // rows side (forward: x, input gradient: dy, weight gradient: dy)
+    const void* b;            // columns side (forward and input gradient: w, weight gradient: x)
+    void* out;
+    const float* a_scale;     // 8-bit operands: [x_rows, ceil(len / 128)], [n, ceil(cols / 128), ceil(len / 128)]
+    const float* b_scale;
+    const int32_t* offsets;   // [n + 1] (NULL: one group of all R rows); held inside [0, R] by the kernels
+    const int32_t* gather;    // row of x behind each row (NULL: itself)
+    int64_t x_rows;           // rows of x (gathered indices are clamped to it)
+    int64_t R;                // rows, below 2^30
+    int n;
+    int len;                  // contraction (weight gradient: unused, a group's rows)
+    int cols;                 // columns of out
+    int rows;                 // weight gradient: rows of a group's out
+    int accumulate;           // weight gradient: add into out
+};
+hipError_t launch_grouped(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s);
+hipError_t launch_grouped_dx(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s);
+hipError_t launch_grouped_dw(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s);
+hipError_t launch_grouped_fp8(bool out_bf16, const GroupArgs& g, hipStream_t s);
+// out[t, :] = sum over the slots a ascending of rows[row_of[t, a], :] (float32; negative indices: none).
+hipError_t launch_slot_sum(const float* rows, const int32_t* row_of, int64_t T, int k, int64_t R, int K, void* out,
+                           bool out_bf16, hipStream_t s);
+
+// 8-bit values with a scale for each block of 128 (fp8.hip). swiglu: x holds gate and up halves of 2 K.
+hipError_t launch_quant_rows(bool bf16, bool swiglu, const void* x, const int32_t* count, int64_t R, int K, uint8_t* q,
+                             float* scale, hipStream_t s);
+hipError_t launch_quant_weights(bool bf16, const void* w, int n, int N, int K, uint8_t* q, float* scale, uint8_t* q_t,
+                                float* scale_t, hipStream_t s);
+
 }  // namespace pcm

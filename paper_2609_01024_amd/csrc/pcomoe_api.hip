@@ -59,6 +59,24 @@ pcm_status check_paths(const pcm_paths* p) {
     return PCM_OK;
 }
 
+// The experts' products: sizes, then types.
+constexpr int64_t kMaxGroupedRows = (int64_t)1 << 30;
+pcm_status check_grouped(int64_t T, int64_t R, int K, int N, int n) {
+    if (T < 0 || R < 0 || K < 1 || N < 1 || n < 1) return PCM_ERR_ARG;
+    if (K % 16 || N % 16 || n > kMaxN || T >= kMaxGroupedRows || R >= kMaxGroupedRows) return PCM_ERR_UNSUPPORTED;
+    return PCM_OK;
+}
+bool plain_dtype(pcm_dtype d) { return d == PCM_F32 || d == PCM_BF16; }
+bool grouped_types(pcm_dtype dtype, pcm_dtype out) {
+    return plain_dtype(dtype) && plain_dtype(out) && (dtype == PCM_BF16 || out == PCM_F32);
+}
+// The rows of a product: without offsets one group, without a gather the rows themselves.
+bool grouped_rows(const int32_t* offsets, const int32_t* row_token, int64_t T, int64_t R, int n) {
+    if (!offsets && (n != 1 || row_token)) return false;
+    if (!row_token && T != R) return false;
+    return !(row_token && T == 0 && R > 0) && aligned16(offsets) && aligned16(row_token);
+}
+
 pcm_status from_hip(hipError_t e) { return e == hipSuccess ? PCM_OK : PCM_ERR_HIP; }
 
 pcm_status check_scored(const pcm_scored_paths* p) {
@@ -160,7 +178,7 @@ const char* pcm_status_string(pcm_status s) {
     switch (s) {
         case PCM_OK: return "PCM_OK: success";
         case PCM_ERR_ARG: return "PCM_ERR_ARG: invalid argument (null or misaligned pointer, bad size, k > n)";
-        case PCM_ERR_UNSUPPORTED: return "PCM_ERR_UNSUPPORTED: outside the supported limits (k <= 8, n <= 256, H and F multiples of 64, T*k < 2^31)";
+        case PCM_ERR_UNSUPPORTED: return "PCM_ERR_UNSUPPORTED: outside the supported limits (k <= 8, n <= 256, H and F multiples of 64, T*k < 2^31; experts' products: K and N multiples of 16, T and R < 2^30)";
         case PCM_ERR_WORKSPACE: return "PCM_ERR_WORKSPACE: workspace smaller than pcm_workspace_bytes()";
         case PCM_ERR_HIP: return "PCM_ERR_HIP: a HIP launch failed";
     }
@@ -182,6 +200,9 @@ size_t pcm_workspace_bytes(pcm_op op, int64_t T, int H, int F, int n, int k, pcm
         case PCM_OP_LAYER_PER_PATH:
             if (H < 1 || F < 1) return 0;
             return path_ws(T, H, F, n, k, dtype).total;
+        case PCM_OP_GROUPED_DX:  // the rows' gradients [T*k, K] f32, K in the place of H
+            if (H < 1) return 0;
+            return align_up((size_t)T * k * H * sizeof(float), 256);
         case PCM_OP_ROUTE_SCORED:  // block counts of the source and the target dispatch
             return 2 * build_paths_ws_bytes(T, n);
         case PCM_OP_DENSE_SWIGLU:  // the SwiGLU output u [T,F] f32, then a projection input
@@ -725,6 +746,150 @@ pcm_status pcm_project_combine_scored(pcm_dtype dtype, const void* u, const void
                                       void* stream) {
     return pcm_project_combine_scored_tuned(dtype, u, w_down, paths, T, H, F, n, K, y, accumulate,
                                             ws, ws_bytes, stream, nullptr);
+}
+
+pcm_status pcm_grouped_gemm(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const void* w,
+                            const int32_t* offsets, const int32_t* row_token, int64_t T, int64_t R,
+                            int K, int N, int n, void* y, void* stream) {
+    const pcm_status st = check_grouped(T, R, K, N, n);
+    if (st != PCM_OK) return st;
+    if (!grouped_types(dtype, out_dtype)) return PCM_ERR_ARG;
+    if (!grouped_rows(offsets, row_token, T, R, n)) return PCM_ERR_ARG;
+    if (R == 0) return PCM_OK;
+    if (!x || !w || !y || !aligned16(x) || !aligned16(w) || !aligned16(y)) return PCM_ERR_ARG;
+    GroupArgs g{};
+    g.a = x;
+    g.b = w;
+    g.out = y;
+    g.offsets = offsets;
+    g.gather = row_token;
+    g.x_rows = T;
+    g.R = R;
+    g.n = n;
+    g.len = K;
+    g.cols = N;
+    return from_hip(launch_grouped(dtype == PCM_BF16, out_dtype == PCM_BF16, g, (hipStream_t)stream));
+}
+
+pcm_status pcm_grouped_gemm_dx(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* w,
+                               const int32_t* offsets, const int32_t* row_of, int64_t T, int k,
+                               int64_t R, int K, int N, int n, void* dx, void* ws, size_t ws_bytes,
+                               void* stream) {
+    const pcm_status st = check_grouped(T, R, K, N, n);
+    if (st != PCM_OK) return st;
+    if (!grouped_types(dtype, out_dtype) || k < 1) return PCM_ERR_ARG;
+    if (k > kMaxK) return PCM_ERR_UNSUPPORTED;
+    if (!grouped_rows(offsets, nullptr, R, R, n)) return PCM_ERR_ARG;
+    if (row_of ? R > T * k : T != R || k != 1) return PCM_ERR_ARG;
+    if (T == 0) return PCM_OK;
+    if (!dx || !aligned16(dx) || !aligned16(row_of)) return PCM_ERR_ARG;
+    if (R > 0 && (!dy || !w || !aligned16(dy) || !aligned16(w))) return PCM_ERR_ARG;
+    if (row_of) {
+        const size_t need = pcm_workspace_bytes(PCM_OP_GROUPED_DX, T, K, 0, n, k, dtype);
+        if (ws_bytes < need || !ws) return PCM_ERR_WORKSPACE;
+        if (!aligned16(ws)) return PCM_ERR_ARG;
+    }
+    GroupArgs g{};
+    g.a = dy;
+    g.b = w;
+    g.out = row_of ? ws : dx;
+    g.offsets = offsets;
+    g.x_rows = R;
+    g.R = R;
+    g.n = n;
+    g.len = N;
+    g.cols = K;
+    hipStream_t s = (hipStream_t)stream;
+    if (R > 0) {
+        const hipError_t err = launch_grouped_dx(dtype == PCM_BF16, !row_of && out_dtype == PCM_BF16, g, s);
+        if (err != hipSuccess) return PCM_ERR_HIP;
+    }
+    if (!row_of) return PCM_OK;
+    return from_hip(launch_slot_sum((const float*)ws, row_of, T, k, R, K, dx, out_dtype == PCM_BF16, s));
+}
+
+pcm_status pcm_grouped_gemm_dw(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const void* dy,
+                               const int32_t* offsets, const int32_t* row_token, int64_t T, int64_t R,
+                               int K, int N, int n, void* dw, int accumulate, void* stream) {
+    const pcm_status st = check_grouped(T, R, K, N, n);
+    if (st != PCM_OK) return st;
+    if (!grouped_types(dtype, out_dtype) || (accumulate && out_dtype != PCM_F32)) return PCM_ERR_ARG;
+    if (!grouped_rows(offsets, row_token, T, R, n)) return PCM_ERR_ARG;
+    if (!dw || !aligned16(dw)) return PCM_ERR_ARG;
+    if (R > 0 && (!x || !dy || !aligned16(x) || !aligned16(dy))) return PCM_ERR_ARG;
+    if (R == 0 && accumulate) return PCM_OK;
+    GroupArgs g{};
+    g.a = dy;
+    g.b = x;
+    g.out = dw;
+    g.offsets = R > 0 ? offsets : nullptr;
+    g.gather = R > 0 ? row_token : nullptr;
+    g.x_rows = T;
+    g.R = R;
+    g.n = n;
+    g.rows = N;
+    g.cols = K;
+    g.accumulate = accumulate != 0;
+    return from_hip(launch_grouped_dw(dtype == PCM_BF16, out_dtype == PCM_BF16, g, (hipStream_t)stream));
+}
+
+static pcm_status quant_rows(pcm_dtype dtype, bool swiglu, const void* x, const int32_t* count, int64_t R,
+                             int K, uint8_t* q, float* scale, void* stream) {
+    const pcm_status st = check_grouped(0, R, K, 16, 1);
+    if (st != PCM_OK) return st;
+    if (!plain_dtype(dtype)) return PCM_ERR_ARG;
+    if (R == 0) return PCM_OK;
+    // count may be any element of an offsets array
+    if (!x || !q || !scale || !aligned16(x) || !aligned16(q) || !aligned16(scale) || ((uintptr_t)count & 3u))
+        return PCM_ERR_ARG;
+    return from_hip(launch_quant_rows(dtype == PCM_BF16, swiglu, x, count, R, K, q, scale, (hipStream_t)stream));
+}
+
+pcm_status pcm_quant_fp8_rows(pcm_dtype dtype, const void* x, const int32_t* count, int64_t R, int K,
+                              uint8_t* q, float* scale, void* stream) {
+    return quant_rows(dtype, false, x, count, R, K, q, scale, stream);
+}
+
+pcm_status pcm_swiglu_quant_fp8(pcm_dtype dtype, const void* gate_up, const int32_t* count, int64_t R,
+                                int F, uint8_t* q, float* scale, void* stream) {
+    return quant_rows(dtype, true, gate_up, count, R, F, q, scale, stream);
+}
+
+pcm_status pcm_quant_fp8_weights(pcm_dtype dtype, const void* w, int n, int N, int K, uint8_t* q,
+                                 float* scale, uint8_t* q_t, float* scale_t, void* stream) {
+    const pcm_status st = check_grouped(0, 0, K, N, n);
+    if (st != PCM_OK) return st;
+    if (!plain_dtype(dtype)) return PCM_ERR_ARG;
+    if (!w || !q || !scale || !aligned16(w) || !aligned16(q) || !aligned16(scale)) return PCM_ERR_ARG;
+    if (!q_t != !scale_t || !aligned16(q_t) || !aligned16(scale_t)) return PCM_ERR_ARG;
+    return from_hip(launch_quant_weights(dtype == PCM_BF16, w, n, N, K, q, scale, q_t, scale_t, (hipStream_t)stream));
+}
+
+pcm_status pcm_grouped_gemm_fp8(pcm_dtype out_dtype, const uint8_t* x, const float* x_scale,
+                                const uint8_t* w, const float* w_scale, const int32_t* offsets,
+                                const int32_t* row_token, int64_t T, int64_t R, int K, int N, int n,
+                                void* y, void* stream) {
+    const pcm_status st = check_grouped(T, R, K, N, n);
+    if (st != PCM_OK) return st;
+    if (!plain_dtype(out_dtype) || !grouped_rows(offsets, row_token, T, R, n)) return PCM_ERR_ARG;
+    if (R == 0) return PCM_OK;
+    if (!x || !x_scale || !w || !w_scale || !y) return PCM_ERR_ARG;
+    if (!aligned16(x) || !aligned16(x_scale) || !aligned16(w) || !aligned16(w_scale) || !aligned16(y))
+        return PCM_ERR_ARG;
+    GroupArgs g{};
+    g.a = x;
+    g.b = w;
+    g.a_scale = x_scale;
+    g.b_scale = w_scale;
+    g.out = y;
+    g.offsets = offsets;
+    g.gather = row_token;
+    g.x_rows = T;
+    g.R = R;
+    g.n = n;
+    g.len = K;
+    g.cols = N;
+    return from_hip(launch_grouped_fp8(out_dtype == PCM_BF16, g, (hipStream_t)stream));
 }
 
 }  // extern "C"
