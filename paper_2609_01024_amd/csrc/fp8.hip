@@ -149,7 +149,17 @@ __global__ __launch_bounds__(256) void quant_weights_kernel(const IN* __restrict
     }
 }
 
-using Small = TileCfg<64, 64, 2, 2, 3>;
+using Small = TileCfg<64, 64, 2, 2, 3>;      // three workgroups on a compute unit
+using Wide = TileCfg<128, 256, 2, 4, 3>;     // one, eight waves of 64 x 64
+
+template <class E, class OUT>
+hipError_t fp8_by_shape(const GroupArgs& g, hipStream_t s) {
+    if (!near(g, 1)) return launch_rows<E, Small, Small, false, OUT, int64_t>(g, 8, s);
+    auto tiles = [&](int bm, int bn) { return expected_row_tiles(g, bm) * ceil_div(g.cols, bn); };
+    if (mean_rows(g) <= 16 || tiles(16, 64) <= 256) return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, E::SIZE), s);
+    if (tiles(128, 256) >= 56) return launch_rows<E, Wide, Wide, false, OUT>(g, 8, s);
+    return launch_rows<E, Small, Small, false, OUT>(g, 8, s);
+}
 
 }  // namespace
 
@@ -181,7 +191,7 @@ hipError_t launch_quant_weights(bool bf16, const void* w, int n, int N, int K, u
 }
 
 hipError_t launch_grouped_fp8(bool out_bf16, const GroupArgs& g, hipStream_t s) {
-    return out_bf16 ? launch_rows<TE4m3, Small, false, __bf16>(g, 8, s) : launch_rows<TE4m3Wide, Small, false, float>(g, 8, s);
+    return out_bf16 ? fp8_by_shape<TE4m3, __bf16>(g, s) : fp8_by_shape<TE4m3Wide, float>(g, s);
 }
 
 }  // namespace pcm

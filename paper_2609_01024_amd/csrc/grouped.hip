@@ -8,11 +8,27 @@
 namespace pcm {
 namespace {
 
-using Small = TileCfg<64, 64, 2, 2, 3>;
+using Small = TileCfg<64, 64, 2, 2, 3>;          // three workgroups on a compute unit
+using Middle = TileCfg<64, 128, 2, 2, 3>;        // two
+using Square = TileCfg<128, 128, 2, 2, 2, 3>;    // two
+using Large = TileCfg<256, 256, 2, 4, 2, 3>;     // one, eight waves of 128 x 64
+using LargeTail = TileCfg<128, 256, 2, 4, 2, 3>;
 
 template <class E, bool DX, class OUT>
 hipError_t rows_by_shape(const GroupArgs& g, hipStream_t s) {
-    return launch_rows<E, Small, DX, OUT>(g, 8, s);
+    if (!near(g, E::SIZE)) return launch_rows<E, Small, Small, DX, OUT, int64_t>(g, 8, s);
+    auto tiles = [&](int bm, int bn) { return expected_row_tiles(g, bm) * ceil_div(g.cols, bn); };
+    if constexpr (E::SIZE == 4) {
+        return launch_rows<E, Small, Small, DX, OUT>(g, 8, s);
+    } else {
+        if constexpr (!DX)
+            if (mean_rows(g) <= 16 || tiles(16, 64) <= 256)
+                return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, E::SIZE), s);
+        if (tiles(256, 256) >= 192) return launch_rows<E, Large, LargeTail, DX, OUT>(g, 8, s);
+        if (tiles(128, 128) >= 256) return launch_rows<E, Square, Square, DX, OUT>(g, 8, s);
+        if (tiles(64, 128) >= 256) return launch_rows<E, Middle, Middle, DX, OUT>(g, 8, s);
+        return launch_rows<E, Small, Small, DX, OUT>(g, 8, s);
+    }
 }
 
 template <bool DX>
@@ -23,6 +39,12 @@ hipError_t rows_by_type(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_
 
 template <class E, class OUT, bool ADD>
 hipError_t outer_by_shape(const GroupArgs& g, hipStream_t s) {
+    if (!near(g, E::SIZE)) return launch_outer<E, Small, OUT, ADD, int64_t>(g, s);
+    auto tiles = [&](int bm, int bn) { return g.n * ceil_div(g.rows, bm) * ceil_div(g.cols, bn); };
+    if constexpr (E::SIZE == 2) {
+        if (tiles(256, 256) >= 192) return launch_outer<E, Large, OUT, ADD>(g, s);
+        if (tiles(128, 128) >= 128) return launch_outer<E, Square, OUT, ADD>(g, s);
+    }
     return launch_outer<E, Small, OUT, ADD>(g, s);
 }
 

@@ -210,6 +210,125 @@ def test_gradients_against_differences(types):
     assert float((D * (f(x, w + vw) - f(x, w - vw))).sum()) == 2 * float((dw * vw.double()).sum())
 
 
+# ------------------------------------------------------------------------ every tile
+# Sizes at which each kernel is chosen (by the number of its tiles), contractions of one to many slices of
+# every kind: whole, cut, and around the eight slices whose 8-bit scales travel together.
+LENGTHS = [16, 64, 80, 128, 144, 192, 208, 320, 400, 1040, 1168, 2064]
+TILES = {   # counts, columns
+    "256 x 256": ([700, 1500, 130, 0, 670, 257], 4112),
+    "128 x 128": ([1000], 4112),
+    "64 x 128": ([129, 1, 370], 4112),
+    "64 x 64": ([90, 33, 40], 272),
+    "16 rows": ([16, 1, 0, 17, 5, 40, 3, 2], 208),
+}
+
+
+def on(c):
+    return {k: v.to(DEV) if isinstance(v, torch.Tensor) else v for k, v in c.items()}
+
+
+def rows64(c, a, b, dx=False):
+    """Row-wise products of every group in 64 bits on the GPU, and the sums of magnitudes."""
+    bounds = c["off"].tolist()
+    cols = b.shape[2] if dx else b.shape[1]
+    y = torch.zeros((a.shape[0], cols), dtype=torch.float64, device=DEV)
+    m = torch.zeros_like(y)
+    for i in range(b.shape[0]):
+        r, w = slice(bounds[i], bounds[i + 1]), (b[i] if dx else b[i].T).double().contiguous()
+        y[r] = a[r].double() @ w
+        m[r] = a[r].double().abs() @ w.abs()
+    return y.cpu(), m.cpu()
+
+
+@pytest.mark.parametrize("types", ["bf16-bf16", "bf16-f32", "f32-f32"])
+@pytest.mark.parametrize("length", LENGTHS)
+@pytest.mark.parametrize("tile", TILES)
+def test_tiles_forward_and_input_gradient(tile, length, types):
+    counts, cols = TILES[tile]
+    dt, out = (TYPES[t] for t in types.split("-"))
+    c = on(made((sum(counts), 1, counts, len(counts), length, cols), dt, True, seed=length))
+    y = pcm.pcm_grouped_gemm(c["x"], c["w"], c["off"], c["tok"], out_dtype=out)
+    close(y, *rows64(c, c["x"][c["tok"].long()], c["w"]), length, "y")
+    c = on(made((sum(counts), 1, counts, len(counts), cols, length), dt, False, seed=length))
+    dx = pcm.pcm_grouped_gemm_dx(c["dy"], c["w"], c["off"], out_dtype=out)
+    close(dx, *rows64(c, c["dy"], c["w"], dx=True), length, "dx")
+
+
+@pytest.mark.parametrize("gather", [True, False])
+@pytest.mark.parametrize("types", ["bf16-bf16", "bf16-f32", "f32-f32"])
+@pytest.mark.parametrize("N,K", [(1552, 1296), (848, 528), (80, 144)])
+@pytest.mark.parametrize("counts", [[0, 1, 63, 64, 65, 200], [127, 128, 129, 500, 2, 191], [320, 256, 16, 3, 0, 1100]])
+def test_tiles_weight_gradient(counts, N, K, types, gather):
+    dt, out = (TYPES[t] for t in types.split("-"))
+    c = on(made((sum(counts), 1, counts, len(counts), K, N), dt, gather, seed=N))
+    dw = torch.full((c["n"], N, K), float("nan"), dtype=out, device=DEV)
+    pcm.pcm_grouped_gemm_dw(c["x"], c["dy"], c["off"], c["tok"], dw=dw)
+    x = (c["x"][c["tok"].long()] if gather else c["x"]).double()
+    bounds = c["off"].tolist()
+    parts = [(x[a:b], c["dy"][a:b].double().T.contiguous()) for a, b in zip(bounds, bounds[1:])]
+    want = torch.stack([d @ v for v, d in parts]).cpu()
+    mag = torch.stack([d.abs() @ v.abs() for v, d in parts]).cpu()
+    close(dw, want, mag, max(counts), "dw")
+    if out == torch.float32:
+        again = dw.clone()
+        pcm.pcm_grouped_gemm_dw(c["x"], c["dy"], c["off"], c["tok"], dw=again, accumulate=True)
+        assert torch.equal(again, dw + dw)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("length", LENGTHS)
+@pytest.mark.parametrize("tile", ["128 x 128", "64 x 128", "64 x 64", "16 rows"])
+def test_tiles_of_8_bits(tile, length, out):
+    counts, cols = TILES[tile]
+    c = on(made8((sum(counts), 1, counts, len(counts), length, cols), True, seed=length))
+    y = product8(c, out_dtype=TYPES[out])
+    x = c["xq"].double() * spread(c["xs"], 0, length)
+    w = c["wq"].double() * spread(c["ws"], cols, length, 2)
+    close(y, *rows64(c, x[c["tok"].long()], w), length, "y", EIGHT[out])
+
+
+def test_rows_too_long_for_32_bits():
+    """Contractions and columns so long that offsets within a tile pass 32 bits, in every direction."""
+    K = (1 << 22) + 48
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn((3, K), generator=g, device=DEV).bfloat16()
+    w = torch.randn((16, K), generator=g, device=DEV).bfloat16()
+    X, W = x.double(), w.double()
+    close(pcm.pcm_grouped_gemm(x, w, out_dtype=torch.float32), (X @ W.T).cpu(), (X.abs() @ W.abs().T).cpu(), K, "y")
+    K = (1 << 24) + 48
+    dy = torch.randn((5, 16), generator=g, device=DEV).bfloat16()
+    w = torch.randn((16, K), generator=g, device=DEV).bfloat16()
+    dx = pcm.pcm_grouped_gemm_dx(dy, w, out_dtype=torch.float32)
+    x = torch.randn((5, K), generator=g, device=DEV).bfloat16()
+    dw = pcm.pcm_grouped_gemm_dw(x, dy, out_dtype=torch.float32)
+    D = dy.double()
+    for at in (slice(0, 4096), slice(K // 2, K // 2 + 4096), slice(K - 4096, K)):
+        W, X = w[:, at].double(), x[:, at].double()
+        close(dx[:, at], (D @ W).cpu(), (D.abs() @ W.abs()).cpu(), 16, "dx")
+        close(dw[:, at], (D.T @ X).cpu(), (D.T.abs() @ X.abs()).cpu(), 5, "dw")
+
+
+def test_rows_gathered_past_32_bits():
+    """x of more than 2 GiB, rows from its end."""
+    T, K, N = 70000, 16400, 48
+    x = torch.empty((T, K), dtype=torch.bfloat16, device=DEV)
+    x.view(torch.int16).zero_()
+    tok = torch.tensor([T - 1, 0, 65535, 65600, T - 2, 12345] * 9, dtype=torch.int32, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    for t in set(tok.tolist()):
+        x[t] = torch.randn(K, generator=g, device=DEV).bfloat16()
+    off = torch.tensor([0, 20, len(tok)], dtype=torch.int32, device=DEV)
+    w = torch.randn((2, N, K), generator=g, device=DEV).bfloat16()
+    rows = x[tok.long()]
+    c = dict(off=off)
+    close(pcm.pcm_grouped_gemm(x, w, off, tok, out_dtype=torch.float32), *rows64(c, rows, w), K, "y")
+    dy = torch.randn((len(tok), N), generator=g, device=DEV).bfloat16()
+    dw = pcm.pcm_grouped_gemm_dw(x, dy, off, tok, out_dtype=torch.float32)
+    for i, r in enumerate((slice(0, 20), slice(20, len(tok)))):
+        D, X = dy[r].double().T.contiguous(), rows[r].double()
+        close(dw[i], (D @ X).cpu(), (D.abs() @ X.abs()).cpu(), 34, "dw")
+
+
 # ------------------------------------------------------------------------ rows that do not count
 @pytest.mark.parametrize("types", ["bf16", "f32"])
 def test_rows_behind_the_last_group(types):
