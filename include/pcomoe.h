@@ -91,7 +91,8 @@ typedef enum pcm_op {
     PCM_OP_LAYER_PER_PATH = 5,
     PCM_OP_ROUTE_LOGITS = 6,
     PCM_OP_ROUTE_PATHS = 7,
-    PCM_OP_GROUPED_DX = 8
+    PCM_OP_GROUPED_DX = 8,
+    PCM_OP_GROUPED_DW = 9
 } pcm_op;
 
 /* Path table and grouped dispatch layout of T tokens (caller-owned device buffers).
@@ -341,10 +342,13 @@ pcm_status pcm_grouped_gemm_dx(pcm_dtype dtype, pcm_dtype out_dtype, const void*
 
 /* Gradient by w of pcm_grouped_gemm: dw[e] = [dw[e] +] sum over the rows r of group e of
  * dy[r, :]^T x[s(r), :]. x [T,K], dy [R,N] of `dtype`, dw [n,N,K] of out_dtype. accumulate adds into dw
- * (PCM_F32 only: a sum over calls is held in 32 bits); otherwise an empty group's dw is zero. */
+ * (PCM_F32 only: a sum over calls is held in 32 bits); otherwise an empty group's dw is zero.
+ * ws: pcm_workspace_bytes(PCM_OP_GROUPED_DW, R, K, N, n, 1, dtype) bytes (0 but for many rows and a
+ * small dw, whose rows are summed in parts). */
 pcm_status pcm_grouped_gemm_dw(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const void* dy,
                                const int32_t* offsets, const int32_t* row_token, int64_t T, int64_t R,
-                               int K, int N, int n, void* dw, int accumulate, void* stream);
+                               int K, int N, int n, void* dw, int accumulate, void* ws, size_t ws_bytes,
+                               void* stream);
 
 /* 8-bit values (OCP e4m3: sign, 4 exponent bits, 3 mantissa bits, largest 448, NaN but no infinity) with
  * a float32 scale for each block of 128: the value stands for code * scale. A block whose largest finite

@@ -21,7 +21,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libpcomoe.
 PCM_F32, PCM_BF16, PCM_BF16_F16DOWN = 0, 1, 2
 BETA_SRC_COND, BETA_PRODUCT, BETA_GLOBAL = 0, 1, 2
 OP_BUILD_PATHS, OP_EXPAND, OP_PROJECT_COMBINE, OP_DENSE_SWIGLU, OP_ROUTE_SCORED = 0, 1, 2, 3, 4
-OP_LAYER_PER_PATH, OP_ROUTE_LOGITS, OP_ROUTE_PATHS, OP_GROUPED_DX = 5, 6, 7, 8
+OP_LAYER_PER_PATH, OP_ROUTE_LOGITS, OP_ROUTE_PATHS, OP_GROUPED_DX, OP_GROUPED_DW = 5, 6, 7, 8, 9
 
 EXPORTS = ("pcm_route", "pcm_build_paths", "pcm_expand", "pcm_project_combine",
            "pcm_dense_swiglu", "pcm_workspace_bytes", "pcm_status_string", "pcm_abi_version",
@@ -121,7 +121,7 @@ def lib(path: str = _LIB_PATH) -> ctypes.CDLL:
                                      I, P, SZ, P]
     L.pcm_grouped_gemm.argtypes = [I, I, P, P, P, P, I64, I64, I, I, I, P, P]
     L.pcm_grouped_gemm_dx.argtypes = [I, I, P, P, P, P, I64, I, I64, I, I, I, P, P, SZ, P]
-    L.pcm_grouped_gemm_dw.argtypes = [I, I, P, P, P, P, I64, I64, I, I, I, P, I, P]
+    L.pcm_grouped_gemm_dw.argtypes = [I, I, P, P, P, P, I64, I64, I, I, I, P, I, P, SZ, P]
     L.pcm_quant_fp8_rows.argtypes = [I, P, P, I64, I, P, P, P]
     L.pcm_swiglu_quant_fp8.argtypes = [I, P, P, I64, I, P, P, P]
     L.pcm_quant_fp8_weights.argtypes = [I, P, I, I, I, P, P, P, P, P]

@@ -150,14 +150,21 @@ __global__ __launch_bounds__(256) void quant_weights_kernel(const IN* __restrict
 }
 
 using Small = TileCfg<64, 64, 2, 2, 3>;      // three workgroups on a compute unit
+using Middle = TileCfg<64, 128, 2, 2, 3>;    // two
+using Square = TileCfg<128, 128, 2, 2, 2>;   // two
 using Wide = TileCfg<128, 256, 2, 4, 3>;     // one, eight waves of 64 x 64
 
 template <class E, class OUT>
 hipError_t fp8_by_shape(const GroupArgs& g, hipStream_t s) {
     if (!near(g, 1)) return launch_rows<E, Small, Small, false, OUT, int64_t>(g, 8, s);
     auto tiles = [&](int bm, int bn) { return expected_row_tiles(g, bm) * ceil_div(g.cols, bn); };
-    if (mean_rows(g) <= 16 || tiles(16, 64) <= 256) return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, E::SIZE), s);
-    if (tiles(128, 256) >= 56) return launch_rows<E, Wide, Wide, false, OUT>(g, 8, s);
+    if (few_rows(g, 1) || tiles(16, 64) <= 256) return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, 1), s);
+    if constexpr (E::PAIRS) {
+        if (tiles(128, 256) >= 56) return launch_rows<E, Wide, Wide, false, OUT>(g, 8, s);
+    } else {
+        if (tiles(128, 128) >= 512 && mean_rows(g) >= 96) return launch_rows<E, Square, Square, false, OUT>(g, 8, s);
+        if (tiles(64, 128) >= 256) return launch_rows<E, Middle, Middle, false, OUT>(g, 8, s);
+    }
     return launch_rows<E, Small, Small, false, OUT>(g, 8, s);
 }
 

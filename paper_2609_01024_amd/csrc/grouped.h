@@ -709,6 +709,14 @@ inline int64_t mean_rows(const GroupArgs& g) {
     const int64_t groups = g.offsets ? (g.R < g.n ? g.R : g.n) : 1;
     return ceil_div(g.R, groups);
 }
+// Whether a mean of few rows a group makes the per-wave rings faster than 64 x 64 tiles and more: enough slices of
+// 128 bytes of the contraction for the rings to run (64 groups, 4096 columns: bf16 54 against 56 us at 8
+// slices, 38 against 31 at 4; 8 bits, mean of 8 rows: 110 against 108 us at 16, 78 against 64 at 8; a mean of 16 rows
+// needs twice as many, the second row tile of some groups reading the weights again).
+inline bool few_rows(const GroupArgs& g, int64_t size) {
+    const int64_t mean = mean_rows(g);
+    return mean <= 16 && ceil_div(g.len * size, 128) >= (size == 1 ? 2 : 1) * (mean > 8 ? 16 : 8);
+}
 // Whether the weights are worth reading non-temporally by groups of one row tile, which read them once:
 // together they are more than half of the 256 MB MALL.
 inline bool weights_once(const GroupArgs& g, int64_t size) {
@@ -791,7 +799,8 @@ __global__ __launch_bounds__(C::NT) void group_rows_kernel(GroupArgs g, int nt, 
     else rows_tile<E, C, DX, OUT, OFF, BYTES>(g, lds, e, row0, row1, ntile);
 }
 
-// out[e] [rows, cols] = sum over the rows r of group e of a[r, :]^T b[s(r), :].
+// out[e] [rows, cols] = sum over the rows r of group e of a[r, :]^T b[s(r), :]. gridDim.y > 1: the rows in that
+// many parts, each with sums of its own, out [parts, n, rows, cols].
 template <class E, class C, bool GATHER, class OUT, bool ADD, class OFF>
 __global__ __launch_bounds__(C::NT) void group_outer_kernel(GroupArgs g, int mt, int nt, int cm, int cn) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -803,7 +812,8 @@ __global__ __launch_bounds__(C::NT) void group_outer_kernel(GroupArgs g, int mt,
     // tiles are 0-3% faster where all groups are alike; the groups sorted by rows first gave 769 us there
     // and cost 5-10% elsewhere, a search in front of every tile).
     const int slots = cm * cn, mc = (mt + cm - 1) / cm, nc = (nt + cn - 1) / cn;
-    const int j8 = (int)(blockIdx.x / 8), chunk = j8 / slots * 8 + (int)(blockIdx.x % 8), slot = j8 % slots;
+    const int j8 = (int)(blockIdx.x / 8), x8 = (int)((blockIdx.x + blockIdx.y) % 8);
+    const int chunk = j8 / slots * 8 + x8, slot = j8 % slots;
     const int e = chunk / (mc * nc), in = chunk - e * (mc * nc);
     const int mtile = in % mc * cm + slot % cm, ntile = in / mc * cn + slot / cm;
     if (e >= g.n || mtile >= mt || ntile >= nt) return;   // workgroup-uniform
@@ -812,6 +822,14 @@ __global__ __launch_bounds__(C::NT) void group_outer_kernel(GroupArgs g, int mt,
         lo = g.offsets[e];
         cnt = g.offsets[e + 1] - lo;
         clamp_group((int)g.R, lo, cnt);
+    }
+    int64_t out = (int64_t)e * g.rows * g.cols;
+    if (gridDim.y > 1) {   // this part of the group's rows, whole slices, into its own sums
+        const int part = ((cnt + E::KB - 1) / E::KB + (int)gridDim.y - 1) / (int)gridDim.y * E::KB;
+        const int skip = min((int)blockIdx.y * part, cnt);
+        lo += skip;
+        cnt = min(part, cnt - skip);
+        out += (int64_t)blockIdx.y * g.n * g.rows * g.cols;
     }
     if (ADD && cnt == 0) return;
     const int64_t ab = (int64_t)g.rows * E::SIZE, bb = (int64_t)g.cols * E::SIZE;
@@ -831,7 +849,7 @@ __global__ __launch_bounds__(C::NT) void group_outer_kernel(GroupArgs g, int mt,
         for (int j = 0; j < C::MB; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     if (cnt > 0)
         tile_loop<E, C, true, true, GATHER, OFF>(A, B, cnt, lds, acc, GATHER ? g.gather + lo : nullptr, g.x_rows, nullptr, nullptr);
-    store_tile<C, OUT, ADD, Slots<E, C>::BYTES>((OUT*)g.out + (int64_t)e * g.rows * g.cols, mtile * C::BM,
+    store_tile<C, OUT, ADD, Slots<E, C>::BYTES>((OUT*)g.out + out, mtile * C::BM,
                                                 g.rows - mtile * C::BM, ntile * C::BN, g.cols, wave, lane, lds, acc);
 }
 
@@ -1010,21 +1028,25 @@ hipError_t launch_thin(const GroupArgs& g, int window, bool once, hipStream_t s)
 }
 
 template <class E, class C, bool GATHER, class OUT, bool ADD, class OFF>
-hipError_t launch_outer_(const GroupArgs& g, hipStream_t s) {
+hipError_t launch_outer_(const GroupArgs& g, int parts, hipStream_t s) {
     const int mt = (int)ceil_div(g.rows, C::BM), nt = (int)ceil_div(g.cols, C::BN);
-    const int cm = mt < 8 ? mt : 8;
-    const int parts = (int)ceil_div((int64_t)nt * cm, 32), cn = (int)ceil_div(nt, parts);
+    // chunks of up to 32 tiles, fewer where that would make less than 64 of them
+    const int64_t some = (int64_t)g.n * mt * nt / 64, most = some < 1 ? 1 : some > 32 ? 32 : some;
+    int cm = 1;   // rows by columns about two to one
+    while (cm < mt && 4 * cm * cm <= 2 * most) cm *= 2;
+    cm = cm < mt ? cm : mt;
+    const int across = (int)ceil_div((int64_t)nt * cm, most), cn = (int)ceil_div(nt, across);
     const int64_t chunks = g.n * ceil_div(mt, cm) * ceil_div(nt, cn), grid = ceil_div(chunks, 8) * 8 * cm * cn;
     if (grid >= int64_t(1) << 28) return hipErrorInvalidValue;
     const auto kernel = group_outer_kernel<E, C, GATHER, OUT, ADD, OFF>;
     const hipError_t err = allow_lds(kernel, Slots<E, C>::BYTES);
     if (err != hipSuccess) return err;
-    kernel<<<dim3((unsigned)grid), dim3(C::NT), Slots<E, C>::BYTES, s>>>(g, mt, nt, cm, cn);
+    kernel<<<dim3((unsigned)grid, (unsigned)parts), dim3(C::NT), Slots<E, C>::BYTES, s>>>(g, mt, nt, cm, cn);
     return hipGetLastError();
 }
 template <class E, class C, class OUT, bool ADD, class OFF = uint32_t>
-hipError_t launch_outer(const GroupArgs& g, hipStream_t s) {
-    return g.gather ? launch_outer_<E, C, true, OUT, ADD, OFF>(g, s) : launch_outer_<E, C, false, OUT, ADD, OFF>(g, s);
+hipError_t launch_outer(const GroupArgs& g, hipStream_t s, int parts = 1) {
+    return g.gather ? launch_outer_<E, C, true, OUT, ADD, OFF>(g, parts, s) : launch_outer_<E, C, false, OUT, ADD, OFF>(g, parts, s);
 }
 
 }  // namespace

@@ -9,6 +9,7 @@ namespace pcm {
 namespace {
 
 using Small = TileCfg<64, 64, 2, 2, 3>;          // three workgroups on a compute unit
+using Narrow = TileCfg<32, 64, 2, 2, 3>;         // float32: four
 using Middle = TileCfg<64, 128, 2, 2, 3>;        // two
 using Square = TileCfg<128, 128, 2, 2, 2, 3>;    // two
 using Large = TileCfg<256, 256, 2, 4, 2, 3>;     // one, eight waves of 128 x 64
@@ -19,10 +20,11 @@ hipError_t rows_by_shape(const GroupArgs& g, hipStream_t s) {
     if (!near(g, E::SIZE)) return launch_rows<E, Small, Small, DX, OUT, int64_t>(g, 8, s);
     auto tiles = [&](int bm, int bn) { return expected_row_tiles(g, bm) * ceil_div(g.cols, bn); };
     if constexpr (E::SIZE == 4) {
+        if (tiles(64, 64) < 1024) return launch_rows<E, Narrow, Narrow, DX, OUT>(g, 8, s);
         return launch_rows<E, Small, Small, DX, OUT>(g, 8, s);
     } else {
         if constexpr (!DX)
-            if (mean_rows(g) <= 16 || tiles(16, 64) <= 256)
+            if (few_rows(g, E::SIZE) || tiles(16, 64) <= 256)
                 return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, E::SIZE), s);
         if (tiles(256, 256) >= 192) return launch_rows<E, Large, LargeTail, DX, OUT>(g, 8, s);
         if (tiles(128, 128) >= 256) return launch_rows<E, Square, Square, DX, OUT>(g, 8, s);
@@ -48,19 +50,45 @@ hipError_t outer_by_shape(const GroupArgs& g, hipStream_t s) {
     return launch_outer<E, Small, OUT, ADD>(g, s);
 }
 
-// A thread adds four columns of a token's rows, slots ascending, in float32.
+// out = [out +] the parts' sums, in order.
+template <class OUT>
+__global__ __launch_bounds__(256) void part_sum_kernel(const float* __restrict__ parts, int count, int64_t size,
+                                                       OUT* __restrict__ out, int add) {
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
+        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < count; p += 8) {   // eight loads in flight; past the end the last again, not added
+            floatx4 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = *(const floatx4*)(parts + min(p + j, count - 1) * size + i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (p + j < count) sum += v[j];
+        }
+        if constexpr (sizeof(OUT) == 4)
+            if (add) sum += *(const floatx4*)(out + i);
+        store4(out + i, sum);
+    }
+}
+
+// A thread adds four columns of a token's rows, slots ascending, in float32. All indices, then all rows, are
+// loaded before any is used.
 template <class OUT>
 __global__ __launch_bounds__(256) void slot_sum_kernel(const float* __restrict__ rows, const int32_t* __restrict__ row_of,
                                                        int64_t T, int k, int64_t R, int K, OUT* __restrict__ out) {
     const int64_t per = K / 4, total = T * per;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t t = i / per, c = (i - t * per) * 4;
+        int r[kMaxK];
+        floatx4 v[kMaxK];
+#pragma unroll
+        for (int a = 0; a < kMaxK; ++a) r[a] = a < k && R > 0 ? row_of[t * k + a] : -1;
+#pragma unroll
+        for (int a = 0; a < kMaxK; ++a)
+            if (r[a] >= 0) v[a] = *(const floatx4*)(rows + min((int64_t)r[a], R - 1) * K + c);
         floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-        for (int a = 0; a < k; ++a) {
-            const int64_t r = row_of[t * k + a];
-            if (r < 0 || R == 0) continue;
-            sum += *(const floatx4*)(rows + (r < R ? r : R - 1) * K + c);
-        }
+#pragma unroll
+        for (int a = 0; a < kMaxK; ++a)
+            if (r[a] >= 0) sum += v[a];
         store4(out + t * K + c, sum);
     }
 }
@@ -75,7 +103,29 @@ hipError_t launch_grouped_dx(bool bf16, bool out_bf16, const GroupArgs& g, hipSt
     return rows_by_type<true>(bf16, out_bf16, g, s);
 }
 
-hipError_t launch_grouped_dw(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s) {
+// Long sums over rows in few tiles (a router's weight, one small matrix) would leave most compute units idle:
+// their rows are cut into parts of at least 256, for at most about two workgroups on each.
+int dw_parts(int64_t R, int N, int K, int n) {
+    const int64_t tiles = n * ceil_div(N, 64) * ceil_div(K, 64), mean = R / n;
+    if (tiles > 128 || mean < 512) return 1;
+    const int64_t parts = 512 / tiles;
+    return (int)(parts < mean / 256 ? parts : mean / 256);
+}
+
+hipError_t launch_grouped_dw(bool bf16, bool out_bf16, const GroupArgs& g, float* ws, hipStream_t s) {
+    const int parts = dw_parts(g.R, g.rows, g.cols, g.n);
+    if (parts > 1 && near(g, bf16 ? 2 : 4)) {
+        GroupArgs p = g;
+        p.out = ws;
+        const hipError_t err = bf16 ? launch_outer<TBf16, Small, float, false>(p, s, parts)
+                                    : launch_outer<TF32, Small, float, false>(p, s, parts);
+        if (err != hipSuccess) return err;
+        const int64_t size = (int64_t)g.n * g.rows * g.cols;
+        const dim3 grid((unsigned)ceil_div(size, 1024));
+        if (out_bf16) part_sum_kernel<<<grid, dim3(256), 0, s>>>(ws, parts, size, (__bf16*)g.out, 0);
+        else part_sum_kernel<<<grid, dim3(256), 0, s>>>(ws, parts, size, (float*)g.out, g.accumulate);
+        return hipGetLastError();
+    }
     if (!bf16) return g.accumulate ? outer_by_shape<TF32, float, true>(g, s) : outer_by_shape<TF32, float, false>(g, s);
     if (out_bf16) return outer_by_shape<TBf16, __bf16, false>(g, s);
     return g.accumulate ? outer_by_shape<TBf16, float, true>(g, s) : outer_by_shape<TBf16, float, false>(g, s);

@@ -274,7 +274,9 @@ struct GroupArgs {
 };
 hipError_t launch_grouped(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s);
 hipError_t launch_grouped_dx(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s);
-hipError_t launch_grouped_dw(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_t s);
+// (ws: dw_parts sums of out's size where there is more than one)
+hipError_t launch_grouped_dw(bool bf16, bool out_bf16, const GroupArgs& g, float* ws, hipStream_t s);
+int dw_parts(int64_t R, int N, int K, int n);
 hipError_t launch_grouped_fp8(bool out_bf16, const GroupArgs& g, hipStream_t s);
 // out[t, :] = sum over the slots a ascending of rows[row_of[t, a], :] (float32; negative indices: none).
 hipError_t launch_slot_sum(const float* rows, const int32_t* row_of, int64_t T, int k, int64_t R, int K, void* out,

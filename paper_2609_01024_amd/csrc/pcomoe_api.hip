@@ -203,6 +203,11 @@ size_t pcm_workspace_bytes(pcm_op op, int64_t T, int H, int F, int n, int k, pcm
         case PCM_OP_GROUPED_DX:  // the rows' gradients [T*k, K] f32, K in the place of H
             if (H < 1) return 0;
             return align_up((size_t)T * k * H * sizeof(float), 256);
+        case PCM_OP_GROUPED_DW: {  // T*k rows, K and N in the places of H and F: the parts' sums
+            if (H < 1 || F < 1) return 0;
+            const int parts = dw_parts(T * k, F, H, n);
+            return parts > 1 ? (size_t)parts * n * H * F * sizeof(float) : 0;
+        }
         case PCM_OP_ROUTE_SCORED:  // block counts of the source and the target dispatch
             return 2 * build_paths_ws_bytes(T, n);
         case PCM_OP_DENSE_SWIGLU:  // the SwiGLU output u [T,F] f32, then a projection input
@@ -810,7 +815,8 @@ pcm_status pcm_grouped_gemm_dx(pcm_dtype dtype, pcm_dtype out_dtype, const void*
 
 pcm_status pcm_grouped_gemm_dw(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const void* dy,
                                const int32_t* offsets, const int32_t* row_token, int64_t T, int64_t R,
-                               int K, int N, int n, void* dw, int accumulate, void* stream) {
+                               int K, int N, int n, void* dw, int accumulate, void* ws, size_t ws_bytes,
+                               void* stream) {
     const pcm_status st = check_grouped(T, R, K, N, n);
     if (st != PCM_OK) return st;
     if (!grouped_types(dtype, out_dtype) || (accumulate && out_dtype != PCM_F32)) return PCM_ERR_ARG;
@@ -818,6 +824,9 @@ pcm_status pcm_grouped_gemm_dw(pcm_dtype dtype, pcm_dtype out_dtype, const void*
     if (!dw || !aligned16(dw)) return PCM_ERR_ARG;
     if (R > 0 && (!x || !dy || !aligned16(x) || !aligned16(dy))) return PCM_ERR_ARG;
     if (R == 0 && accumulate) return PCM_OK;
+    const size_t need = pcm_workspace_bytes(PCM_OP_GROUPED_DW, R, K, N, n, 1, dtype);
+    if (ws_bytes < need || (need && !ws)) return PCM_ERR_WORKSPACE;
+    if (need && !aligned16(ws)) return PCM_ERR_ARG;
     GroupArgs g{};
     g.a = dy;
     g.b = x;
@@ -830,7 +839,8 @@ pcm_status pcm_grouped_gemm_dw(pcm_dtype dtype, pcm_dtype out_dtype, const void*
     g.rows = N;
     g.cols = K;
     g.accumulate = accumulate != 0;
-    return from_hip(launch_grouped_dw(dtype == PCM_BF16, out_dtype == PCM_BF16, g, (hipStream_t)stream));
+    return from_hip(launch_grouped_dw(dtype == PCM_BF16, out_dtype == PCM_BF16, g, (float*)ws,
+                                      (hipStream_t)stream));
 }
 
 static pcm_status quant_rows(pcm_dtype dtype, bool swiglu, const void* x, const int32_t* count, int64_t R,

@@ -12,7 +12,7 @@ from typing import Optional
 
 import torch
 
-from .binding import OP_GROUPED_DX, PCM_BF16, PCM_F32, _check, _on, lib, workspace_bytes
+from .binding import OP_GROUPED_DW, OP_GROUPED_DX, PCM_BF16, PCM_F32, _check, _on, lib, workspace_bytes
 
 _CODES = {torch.float32: PCM_F32, torch.bfloat16: PCM_BF16}
 _E4M3 = torch.float8_e4m3fn
@@ -97,6 +97,12 @@ def _out(t, shape, dtype, device, what, stream):
     return t
 
 
+def _workspace(ws, nbytes: int, device, stream):
+    if not nbytes:
+        return None
+    return _out(ws, (nbytes,) if ws is None else ws.shape, torch.uint8, device, "ws", stream)
+
+
 def pcm_grouped_gemm(x: torch.Tensor, w: torch.Tensor, offsets=None, row_token=None, y=None,
                      out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
     """y[r] = x[row_token[r]] w[e]^T for the rows r of group e (row r of x without row_token).
@@ -134,14 +140,10 @@ def pcm_grouped_gemm_dx(dy: torch.Tensor, w: torch.Tensor, offsets=None, row_of=
         T, k = _matrix(row_of, "row_of")
         _operand(row_of, "row_of", torch.int32, None, dev)
         nbytes = workspace_bytes(OP_GROUPED_DX, T, K, 0, n, k, code)
-        if ws is None:
-            with _on(stream):
-                ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
-        else:
-            _operand(ws, "ws", torch.uint8, None, dev)
+    ws = _workspace(ws, nbytes, dev, stream)
     dx = _out(dx, (T, K), out, dev, "dx", stream)
     status = lib().pcm_grouped_gemm_dx(code, _code(out), _ptr(dy), _ptr(w), _ptr(offsets), _ptr(row_of), T, k, R, K, N, n,
-                                     _ptr(dx), _ptr(ws) if nbytes else None, ws.numel() if nbytes else 0,
+                                     _ptr(dx), _ptr(ws), ws.numel() if nbytes else 0,
                                      _stream_on(stream, dev))
     if status:
         _check(status)
@@ -150,9 +152,10 @@ def pcm_grouped_gemm_dx(dy: torch.Tensor, w: torch.Tensor, offsets=None, row_of=
 
 def pcm_grouped_gemm_dw(x: torch.Tensor, dy: torch.Tensor, offsets=None, row_token=None, dw=None,
                         out_dtype: Optional[torch.dtype] = None, accumulate: bool = False,
-                        stream=None) -> torch.Tensor:
+                        ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The gradient by w, [n, N, K] ([N, K] without offsets): the sum of dy[r]^T x[row_token[r]] over the rows
-    of each group, zero for an empty one. accumulate adds into dw, which is then float32."""
+    of each group, zero for an empty one. accumulate adds into dw, which is then float32.
+    ws: workspace_bytes(OP_GROUPED_DW, R, K, N, n, 1, dtype) bytes."""
     T, K = _matrix(x, "x")
     R, N = _matrix(dy, "dy")
     _operand(x, "x")
@@ -167,8 +170,12 @@ def pcm_grouped_gemm_dw(x: torch.Tensor, dy: torch.Tensor, offsets=None, row_tok
         raise ValueError("accumulate needs dw")
     out = dw.dtype if dw is not None and out_dtype is None else out_dtype or x.dtype
     dw = _out(dw, (n, N, K) if offsets is not None or (dw is not None and dw.dim() == 3) else (N, K), out, dev, "dw", stream)
-    status = lib().pcm_grouped_gemm_dw(_code(x.dtype), _code(out), _ptr(x), _ptr(dy), _ptr(offsets), _ptr(row_token), T, R,
-                                     K, N, n, _ptr(dw), int(bool(accumulate)), _stream_on(stream, dev))
+    code = _code(x.dtype)
+    nbytes = workspace_bytes(OP_GROUPED_DW, R, K, N, n, 1, code)
+    ws = _workspace(ws, nbytes, dev, stream)
+    status = lib().pcm_grouped_gemm_dw(code, _code(out), _ptr(x), _ptr(dy), _ptr(offsets), _ptr(row_token), T, R, K, N, n,
+                                       _ptr(dw), int(bool(accumulate)), _ptr(ws), ws.numel() if nbytes else 0,
+                                       _stream_on(stream, dev))
     if status:
         _check(status)
     return dw

@@ -28,8 +28,8 @@ def grad_x(dt=BF16, out=BF16, dy=P, w=P, off=P, of=P, T=8, k=2, R=16, K=64, N=32
     return (dt, out, dy, w, off, of, T, k, R, K, N, n, dx, ws, wsb, None)
 
 
-def grad_w(dt=BF16, out=BF16, x=P, dy=P, off=P, tok=P, T=8, R=16, K=64, N=32, n=4, dw=P, acc=0):
-    return (dt, out, x, dy, off, tok, T, R, K, N, n, dw, acc, None)
+def grad_w(dt=BF16, out=BF16, x=P, dy=P, off=P, tok=P, T=8, R=16, K=64, N=32, n=4, dw=P, acc=0, ws=None, wsb=0):
+    return (dt, out, x, dy, off, tok, T, R, K, N, n, dw, acc, ws, wsb, None)
 
 
 def eight_bit(out=BF16, x=P, xs=P, w=P, ws=P, off=P, tok=P, T=8, R=16, K=64, N=32, n=4, y=P):
@@ -92,6 +92,17 @@ def test_input_gradient(L):
     assert L.pcm_grouped_gemm_dx(*grad_x(wsb=need - 1)) == WS
     assert L.pcm_grouped_gemm_dx(*grad_x(ws=None)) == WS
     assert L.pcm_grouped_gemm_dx(*grad_x(ws=MIS)) == ARG
+
+
+def test_weight_gradient_workspace(L):
+    """Many rows and a small result: parts of the rows, each with sums of its own."""
+    assert L.pcm_workspace_bytes(binding.OP_GROUPED_DW, 16, 64, 32, 4, 1, BF16) == 0
+    need = L.pcm_workspace_bytes(binding.OP_GROUPED_DW, 8192, 2048, 64, 1, 1, BF16)
+    assert need == 16 * 64 * 2048 * 4                      # 32 tiles: 512 / 32 parts
+    args = dict(off=None, tok=None, n=1, T=8192, R=8192, K=2048, N=64)
+    assert L.pcm_grouped_gemm_dw(*grad_w(**args, ws=P, wsb=need - 1)) == WS
+    assert L.pcm_grouped_gemm_dw(*grad_w(**args, ws=None, wsb=need)) == WS
+    assert L.pcm_grouped_gemm_dw(*grad_w(**args, ws=MIS, wsb=need)) == ARG
 
 
 def test_accumulate_is_float32(L):

@@ -257,7 +257,8 @@ def test_tiles_forward_and_input_gradient(tile, length, types):
 @pytest.mark.parametrize("gather", [True, False])
 @pytest.mark.parametrize("types", ["bf16-bf16", "bf16-f32", "f32-f32"])
 @pytest.mark.parametrize("N,K", [(1552, 1296), (848, 528), (80, 144)])
-@pytest.mark.parametrize("counts", [[0, 1, 63, 64, 65, 200], [127, 128, 129, 500, 2, 191], [320, 256, 16, 3, 0, 1100]])
+@pytest.mark.parametrize("counts", [[0, 1, 63, 64, 65, 200], [127, 128, 129, 500, 2, 191], [320, 256, 16, 3, 0, 1100],
+                                    [0, 4097, 1000], [3000]])
 def test_tiles_weight_gradient(counts, N, K, types, gather):
     dt, out = (TYPES[t] for t in types.split("-"))
     c = on(made((sum(counts), 1, counts, len(counts), K, N), dt, gather, seed=N))
