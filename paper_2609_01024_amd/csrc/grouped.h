@@ -694,6 +694,60 @@ __device__ bool group_item(const GroupArgs& g, int nt, int window, int* s_item) 
     return s_item[4] != 0;
 }
 
+// The same with each XCD's eighth of the row tiles of more than TBM rows before its eighth of the shorter ones,
+// which then fill the last round instead of lengthening it: for products of few rounds (Mixtral-shaped down
+// projection, 576 tiles: 954 -> 847 us; with more rounds, or a row tile or two a group, the order above shares
+// operands better: 256 rows each in 64 groups 176 -> 212 us).
+template <int BM, int TBM>
+__device__ bool group_item_long_first(const GroupArgs& g, int nt, int window, int* s_item) {
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x;
+        int lo[4], cnt[4], m[4], tail[4], nl = 0, ns = 0;   // m: long row tiles, tail: 0 or 1 short one
+        group_bounds(g.offsets, g.n, g.R, lane, lo, cnt);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            clamp_group((int)g.R, lo[j], cnt[j]);
+            const int rem = cnt[j] % BM;
+            m[j] = cnt[j] / BM + (rem > TBM ? 1 : 0);
+            tail[j] = rem > 0 && rem <= TBM ? 1 : 0;
+            nl += m[j] * nt;
+            ns += tail[j] * nt;
+        }
+        const int incl = wave_incl_scan_i32(nl), incs = wave_incl_scan_i32(ns);
+        const int total = __builtin_amdgcn_readlane(incl, 63), totals = __builtin_amdgcn_readlane(incs, 63);
+        const int x8 = (int)(blockIdx.x % 8), j8 = (int)(blockIdx.x / 8);
+        const int l0 = (int)((int64_t)x8 * total / 8), l1 = (int)((int64_t)(x8 + 1) * total / 8);
+        const int s0 = (int)((int64_t)x8 * totals / 8), s1 = (int)((int64_t)(x8 + 1) * totals / 8);
+        const bool is_long = j8 < l1 - l0, valid = is_long || j8 - (l1 - l0) < s1 - s0;
+        if (lane == 0) s_item[4] = valid ? 1 : 0;
+        if (valid) {
+            const int id = is_long ? l0 + j8 : s0 + j8 - (l1 - l0);
+            int start = is_long ? incl - nl : incs - ns;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int mm = is_long ? m[j] : tail[j];
+                if (id >= start && id < start + mm * nt) {
+                    const int l = id - start;
+                    const int band = l / (window * nt), lb = l - band * window * nt;
+                    const int bm = min(window, mm - band * window);
+                    int gn = window / bm;
+                    gn = gn > nt ? nt : gn;
+                    const int gsize = gn * bm, grp = lb / gsize, in = lb - grp * gsize;
+                    const int gcols = min(gn, nt - grp * gn), row = in / gcols;
+                    const int r0 = lo[j] + (is_long ? band * window + row : cnt[j] / BM) * BM;
+                    s_item[0] = lane * 4 + j;
+                    s_item[1] = r0;
+                    s_item[2] = min(lo[j] + cnt[j], r0 + BM);
+                    s_item[3] = grp * gn + (in - row * gcols);
+                }
+                start += mm * nt;
+            }
+        }
+    }
+    __syncthreads();
+    return s_item[4] != 0;
+}
+
 // Most row tiles of BM rows that R rows make in n groups.
 inline int64_t most_row_tiles(const GroupArgs& g, int BM) {
     if (!g.offsets) return ceil_div(g.R, BM);
@@ -785,13 +839,17 @@ __device__ __forceinline__ void rows_tile(const GroupArgs& g, char* lds, int e, 
 
 // A row tile of at most CT::BM rows runs as the smaller tile CT (the same columns and waves; CT = C: none).
 template <class E, class C, class CT, bool DX, class OUT, class OFF>
-__global__ __launch_bounds__(C::NT) void group_rows_kernel(GroupArgs g, int nt, int window) {
+__global__ __launch_bounds__(C::NT) void group_rows_kernel(GroupArgs g, int nt, int window, bool long_first) {
     static_assert(CT::NT == C::NT && CT::BN == C::BN && CT::BM <= C::BM, "tail tile");
     constexpr int BYTES = Slots<E, C>::BYTES;
     static_assert(Slots<E, CT>::BYTES <= BYTES, "tail tile");
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     int* const s_item = (int*)lds;   // read into registers before the first loads overwrite it
-    if (!group_item<C::BM>(g, nt, window, s_item)) return;   // workgroup-uniform
+    if (CT::BM < C::BM && long_first) {   // workgroup-uniform branches and returns
+        if (!group_item_long_first<C::BM, CT::BM>(g, nt, window, s_item)) return;
+    } else if (!group_item<C::BM>(g, nt, window, s_item)) {
+        return;
+    }
     const int e = __builtin_amdgcn_readfirstlane(s_item[0]), row0 = __builtin_amdgcn_readfirstlane(s_item[1]);
     const int row1 = __builtin_amdgcn_readfirstlane(s_item[2]), ntile = __builtin_amdgcn_readfirstlane(s_item[3]);
     __syncthreads();
@@ -1009,7 +1067,9 @@ hipError_t launch_rows(const GroupArgs& g, int window, hipStream_t s) {
     const auto kernel = group_rows_kernel<E, C, CT, DX, OUT, OFF>;
     const hipError_t err = allow_lds(kernel, Slots<E, C>::BYTES);
     if (err != hipSuccess) return err;
-    kernel<<<dim3((unsigned)grid), dim3(C::NT), Slots<E, C>::BYTES, s>>>(g, nt, window);
+    // (groups of few row tiles read their weights once for all of them in the other order)
+    const bool long_first = g.offsets && mean_rows(g) >= 512 && expected_row_tiles(g, C::BM) * nt < 4 * 256;
+    kernel<<<dim3((unsigned)grid), dim3(C::NT), Slots<E, C>::BYTES, s>>>(g, nt, window, long_first);
     return hipGetLastError();
 }
 
