@@ -198,7 +198,7 @@ hipError_t launch_quant_weights(bool bf16, const void* w, int n, int N, int K, u
 }
 
 hipError_t launch_grouped_fp8(bool out_bf16, const GroupArgs& g, hipStream_t s) {
-    return out_bf16 ? fp8_by_shape<TE4m3, __bf16>(g, s) : fp8_by_shape<TE4m3Wide, float>(g, s);
+    return out_bf16 ? fp8_by_shape<TE4m3, __bf16>(g, s) : fp8_by_shape<TE4m3AsBf16, float>(g, s);
 }
 
 }  // namespace pcm

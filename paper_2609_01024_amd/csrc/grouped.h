@@ -149,7 +149,7 @@ struct TE4m3 : E4m3 {
     }
 };
 // Results in float32: the values as bf16 (exact), four bf16 MFMAs, float32 sums to the last bit.
-struct TE4m3Wide : E4m3 {
+struct TE4m3AsBf16 : E4m3 {
     static constexpr bool PAIRS = false;
     struct Value {
         bf16x8 v[4];
@@ -184,6 +184,10 @@ struct Slots {   // LDS: NSA slices of A rows, NSB of B rows, then, for 8-bit op
     static_assert(BYTES <= 160 * 1024, "LDS");
 };
 
+// A weight block's scales, the same for a wave, come by scalar loads: a vector load's wait would cover the
+// slices on their way.
+typedef const __attribute__((address_space(4))) float* ScalarPtr;
+
 // Scales of A's rows (those of its loads), fetched for 8 slices at a time: one load a slice would touch a
 // cache line for every row.
 template <class C>
@@ -205,8 +209,8 @@ __device__ __forceinline__ void buffer_to_lds(const char* base, uint32_t voff, i
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
                      :: "s"((uint32_t)(uintptr_t)(PCM_LDS char*)to), "v"(voff), "s"(r), "s"(soff) : "memory", "m0");
     else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :: "s"((uint32_t)(uintptr_t)(PCM_LDS char*)to), "v"(voff), "s"(r), "s"(soff) : "memory", "m0");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                     :: "s"((uint32_t)(uintptr_t)(PCM_LDS char*)to), "v"(voff), "s"(r), "s"(soff) : "memory", "m0");
 }
 __device__ __forceinline__ void global_to_lds(const char* p, char* to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
@@ -318,12 +322,12 @@ struct Step {
 };
 
 // The tile's sums over a contraction of `len` (>= 1) values. GATHER: the B rows k of slice t are the rows
-// gather[t * KB + ..] of B.base (clamped to x_rows); their indices are loaded a slice ahead. sa: this lane's
-// scale of the first slice (8-bit operands), wsc: the wave's.
+// gather[t * KB + ..] of B.base (clamped to x_rows); their indices are loaded a slice ahead. rs, wsc: the scales of
+// 8-bit operands, A's by row and the wave's of B by slice.
 template <class E, class C, bool A_KS, bool B_KS, bool GATHER, class OFF>
 __device__ __forceinline__ void tile_loop(Side<E, C, C::BM, C::QA, A_KS, OFF>& A, Side<E, C, C::BN, C::QB, B_KS, OFF>& B,
                                           int len, char* lds, floatx4 (&acc)[C::NBK][C::MB], const int32_t* gather,
-                                          int64_t x_rows, const RowScales<C>* rs, const float* wsc) {
+                                          int64_t x_rows, const RowScales<C>* rs, ScalarPtr wsc) {
     using L = Slots<E, C>;
     static_assert(!GATHER || B_KS, "rows k are gathered");
     constexpr int PA = C::QA, PB = C::QB, PER = PA + PB + (GATHER ? C::QB : 0);
@@ -478,12 +482,10 @@ __device__ __forceinline__ void tile_loop(Side<E, C, C::BM, C::QA, A_KS, OFF>& A
             a[(mb / 2) & 1][mb & 1] = E::kc2(p + r * 128 + at0, p + r * 128 + at1);
             sc[(mb / 2) & 1][mb & 1] = *(const float*)(scales_of(kt) + (r + r16) * 32);
         };
-        typedef const __attribute__((address_space(4))) float* ScalarPtr;   // scalar loads
-        const ScalarPtr wss = (ScalarPtr)wsc;
-        float ws = wss[0];
+        float ws = wsc[0];
         auto slice = [&](int kt, auto more, auto last) {
             constexpr bool MORE = decltype(more)::value, LAST = decltype(last)::value;
-            const float ws_next = wss[LAST ? kt : kt + 1];
+            const float ws_next = wsc[LAST ? kt : kt + 1];
             const int la = sla, lb = slb;
             floatx4 q[NG][2];     // products, scaled and added two groups later
             float f[2][2];
@@ -568,22 +570,22 @@ __device__ __forceinline__ void tile_loop(Side<E, C, C::BM, C::QA, A_KS, OFF>& A
                 for (int k = 0; k < 4; ++k)
                     acc[C::NBK - 2 + i][C::MB - 2 + j][k] = fmaf(held[i][j][k], held_f[j], acc[C::NBK - 2 + i][C::MB - 2 + j][k]);
     } else {
-    read(f0, 0, 0);
-    int kt = 0;
-    for (; kt + C::NSB < KT - 1; ++kt) slice(kt, std::true_type{});   // whole slices to come
-    for (; kt < KT - 1; ++kt) slice(kt, std::false_type{});
-    if constexpr (E::SCALED) {
-        if (part) f0.head(0, kg, rem);
-        f0.multiply(acc, wsc[KT - 1]);
-    } else {
-        read(f1, 1, 0);
-        if (part) {
-            f0.head(0, kg, rem);
-            f1.head(1, kg, rem);
+        read(f0, 0, 0);
+        int kt = 0;
+        for (; kt + C::NSB < KT - 1; ++kt) slice(kt, std::true_type{});   // whole slices to come
+        for (; kt < KT - 1; ++kt) slice(kt, std::false_type{});
+        if constexpr (E::SCALED) {
+            if (part) f0.head(0, kg, rem);
+            f0.multiply(acc, wsc[KT - 1]);
+        } else {
+            read(f1, 1, 0);
+            if (part) {
+                f0.head(0, kg, rem);
+                f1.head(1, kg, rem);
+            }
+            f0.multiply(acc, 1.0f);
+            f1.multiply(acc, 1.0f);
         }
-        f0.multiply(acc, 1.0f);
-        f1.multiply(acc, 1.0f);
-    }
     }
 }
 
@@ -819,14 +821,14 @@ __device__ __forceinline__ void rows_tile(const GroupArgs& g, char* lds, int e, 
     }
     B.ld = colb;
     RowScales<C> rs;
-    const float* wsc = nullptr;
+    ScalarPtr wsc = nullptr;
     if constexpr (E::SCALED) {
         const int kb = (g.len + 127) / 128, nb = (g.cols + 127) / 128;
         rs.base = g.a_scale + first * kb;
         rs.kb = kb;
 #pragma unroll
         for (int q = 0; q < C::QA; ++q) rs.off[q] = src[q] * kb;
-        wsc = g.b_scale + ((int64_t)e * nb + min((col0 + wave % C::WN * C::WTN) / 128, nb - 1)) * kb;
+        wsc = (ScalarPtr)(g.b_scale + ((int64_t)e * nb + min((col0 + wave % C::WN * C::WTN) / 128, nb - 1)) * kb);
     }
     floatx4 acc[C::NBK][C::MB];
 #pragma unroll
@@ -963,7 +965,6 @@ __global__ __launch_bounds__(NW * 64) void group_thin_kernel(GroupArgs g, int nt
     A.ld = B.ld = 0;
     const int kb = (g.len + 127) / 128, nb128 = (g.cols + 127) / 128;
     const float* xs = E::SCALED ? g.a_scale + scale_row * kb + wave : nullptr;
-    typedef const __attribute__((address_space(4))) float* ScalarPtr;   // scalar loads
     const ScalarPtr ws = E::SCALED ? (ScalarPtr)(g.b_scale + ((int64_t)e * nb128 + col0 / 128) * kb + wave) : nullptr;
     auto issue = [&](int i, int slot) {
         char* S = ring + slot * T::SLOT;
