@@ -37,10 +37,11 @@ __device__ __forceinline__ Eight load8(const float* p) {
     return Eight{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
 
+template <bool FINITE>
 __device__ __forceinline__ uint32_t block_max(const Eight& x) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, finite_bits(x.v[i]));
+    for (int i = 0; i < 8; ++i) m = max(m, FINITE ? finite_bits(x.v[i]) : __float_as_uint(x.v[i]) & 0x7FFFFFFFu);
     return m;
 }
 // largest of the 16 lanes of a DPP row, on each of them
@@ -49,6 +50,12 @@ __device__ __forceinline__ uint32_t row16_max(uint32_t v) {
     v = max(v, dpp_u32<0x4E>(v));
     v = max(v, dpp_u32<0x141>(v));
     return max(v, dpp_u32<0x140>(v));
+}
+
+// The block's largest finite magnitude: all values first, the finite ones again where that finds another.
+__device__ __forceinline__ uint32_t row16_block_max(const Eight& x) {
+    const uint32_t m = row16_max(block_max<false>(x));
+    return __any(m >= 0x7F800000u) ? row16_max(block_max<true>(x)) : m;
 }
 
 __device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d) {
@@ -60,9 +67,16 @@ __device__ __forceinline__ uintx2 eight_e4m3(const Eight& x, float inv) {
                   four_e4m3(x.v[4] * inv, x.v[5] * inv, x.v[6] * inv, x.v[7] * inv)};
 }
 
-// bf16 gates: the hardware exponential and reciprocal (about 1 ulp each, far below e4m3's step);
-// float32 ones: the library exponential and an IEEE division
-__device__ __forceinline__ float gated(uint16_t, float g, float u) { return silu(g) * u; }
+// SiLU(g) u in float32, near to correctly rounded: an error of some units in the last place would move as many
+// more codes across a border between two. bf16 inputs (this is what the kernel has time for next to its
+// memory traffic): e^-g = 2^i 2^f with i whole and f from one fused multiply-add (2^(-g log2 e) at once is off by
+// |g| units), and the hardware reciprocal (about 1 ulp); far below 0 the exponential is inf and the result
+// -0. float32 inputs: the library exponential and an IEEE division.
+__device__ __forceinline__ float gated(uint16_t, float g, float u) {
+    constexpr float kLog2e = 1.44269504088896340736f;
+    const float c = fmaxf(g, -1000.0f), i = rintf(-c * kLog2e), f = fmaf(-c, kLog2e, -i);
+    return g * __builtin_amdgcn_rcpf(1.0f + ldexpf(__builtin_amdgcn_exp2f(f), (int)i)) * u;
+}
 __device__ __forceinline__ float gated(float, float g, float u) { return g / (1.0f + expf(-g)) * u; }
 
 // Rows in blocks of 128 columns: 16 lanes take a block, 8 values each; the maximum stays in registers.
@@ -87,7 +101,7 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const IN* __restrict__ 
                 v = load8(x + r * K + c);
             }
         }
-        const float a = fmaxf(__uint_as_float(row16_max(block_max(v))), kFloor);
+        const float a = fmaxf(__uint_as_float(row16_block_max(v)), kFloor);
         if (c < K) *(uintx2*)(q + r * K + c) = eight_e4m3(v, kE4m3Max / a);
         if (part == 0) scale[b] = a / kE4m3Max;
     }
@@ -114,7 +128,7 @@ __global__ __launch_bounds__(256) void quant_weights_kernel(const IN* __restrict
         const int r = ib * 128 + i * 16 + r0;
         v[i] = Eight{};
         if (r < N && c < K) v[i] = load8(w + (int64_t)r * K + c);
-        m = max(m, block_max(v[i]));
+        m = max(m, block_max<true>(v[i]));
     }
     m = wave_max_u32(m);
     if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = m;
@@ -149,7 +163,8 @@ __global__ __launch_bounds__(256) void quant_weights_kernel(const IN* __restrict
     }
 }
 
-using Small = TileCfg<64, 64, 2, 2, 3>;      // three workgroups on a compute unit
+using Narrow = TileCfg<32, 64, 2, 2, 4>;     // three workgroups on a compute unit
+using Small = TileCfg<64, 64, 2, 2, 3>;      // three
 using Middle = TileCfg<64, 128, 2, 2, 3>;    // two
 using Square = TileCfg<128, 128, 2, 2, 2>;   // two
 using Wide = TileCfg<128, 256, 2, 4, 3>;     // one, eight waves of 64 x 64
@@ -159,8 +174,9 @@ hipError_t fp8_by_shape(const GroupArgs& g, hipStream_t s) {
     if (!near(g, 1)) return launch_rows<E, Small, Small, false, OUT, int64_t>(g, 8, s);
     auto tiles = [&](int bm, int bn) { return expected_row_tiles(g, bm) * ceil_div(g.cols, bn); };
     if (few_rows(g, 1) || tiles(16, 64) <= 256) return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, 1), s);
+    if (tiles(64, 64) <= 256) return launch_rows<E, Narrow, Narrow, false, OUT>(g, 8, s);
     if constexpr (E::PAIRS) {
-        if (tiles(128, 256) >= 56) return launch_rows<E, Wide, Wide, false, OUT>(g, 8, s);
+        if (tiles(128, 256) >= 100) return launch_rows<E, Wide, Wide, false, OUT>(g, 8, s);
     } else {
         if (tiles(128, 128) >= 512 && mean_rows(g) >= 96) return launch_rows<E, Square, Square, false, OUT>(g, 8, s);
         if (tiles(64, 128) >= 256) return launch_rows<E, Middle, Middle, false, OUT>(g, 8, s);

@@ -758,7 +758,7 @@ inline int64_t most_row_tiles(const GroupArgs& g, int BM) {
 
 // Row tiles of BM rows to expect: whole tiles and, for each group with rows, half a tile.
 inline int64_t expected_row_tiles(const GroupArgs& g, int64_t BM) {
-    if (!g.offsets) return ceil_div(g.R, BM);
+    if (g.n == 1) return ceil_div(g.R, BM);
     return g.R / BM + ((g.R < g.n ? g.R : g.n) + 1) / 2;
 }
 inline int64_t mean_rows(const GroupArgs& g) {

@@ -9,7 +9,7 @@ namespace pcm {
 namespace {
 
 using Small = TileCfg<64, 64, 2, 2, 3>;          // three workgroups on a compute unit
-using Narrow = TileCfg<32, 64, 2, 2, 3>;         // float32: four
+using Narrow = TileCfg<32, 64, 2, 2, 4>;         // three
 using Middle = TileCfg<64, 128, 2, 2, 3>;        // two
 using Square = TileCfg<128, 128, 2, 2, 2, 3>;    // two
 using Large = TileCfg<256, 256, 2, 4, 2, 3>;     // one, eight waves of 128 x 64
@@ -26,6 +26,7 @@ hipError_t rows_by_shape(const GroupArgs& g, hipStream_t s) {
         if constexpr (!DX)
             if (few_rows(g, E::SIZE) || tiles(16, 64) <= 256)
                 return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, E::SIZE), s);
+        if (tiles(64, 64) <= 128) return launch_rows<E, Narrow, Narrow, DX, OUT>(g, 8, s);
         if (tiles(256, 256) >= 192) return launch_rows<E, Large, LargeTail, DX, OUT>(g, 8, s);
         if (tiles(128, 128) >= 256) return launch_rows<E, Square, Square, DX, OUT>(g, 8, s);
         if (tiles(64, 128) >= 256) return launch_rows<E, Middle, Middle, DX, OUT>(g, 8, s);

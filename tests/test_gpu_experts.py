@@ -216,9 +216,11 @@ def test_gradients_against_differences(types):
 LENGTHS = [16, 64, 80, 128, 144, 192, 208, 320, 400, 1040, 1168, 2064]
 TILES = {   # counts, columns
     "256 x 256": ([700, 1500, 130, 0, 670, 257], 4112),
+    "256 x 256, short groups": ([300, 20, 129, 500, 64, 77, 255, 256], 6160),
     "128 x 128": ([1000], 4112),
     "64 x 128": ([129, 1, 370], 4112),
-    "64 x 64": ([90, 33, 40], 272),
+    "64 x 64": ([90, 33, 40, 200, 61], 1040),
+    "32 x 64": ([90, 33, 40], 272),
     "16 rows": ([16, 1, 0, 17, 5, 40, 3, 2], 208),
 }
 
@@ -278,7 +280,7 @@ def test_tiles_weight_gradient(counts, N, K, types, gather):
 
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("length", LENGTHS)
-@pytest.mark.parametrize("tile", ["128 x 128", "64 x 128", "64 x 64", "16 rows"])
+@pytest.mark.parametrize("tile", ["128 x 128", "64 x 128", "64 x 64", "32 x 64", "16 rows"])
 def test_tiles_of_8_bits(tile, length, out):
     counts, cols = TILES[tile]
     c = on(made8((sum(counts), 1, counts, len(counts), length, cols), True, seed=length))
@@ -522,6 +524,22 @@ def test_quantise_swiglu_rows(R, F, types):
     wide = s.repeat_interleave(128, 1)[:, :F]
     d = (q.cpu().double() * scale.cpu().double().repeat_interleave(128, 1)[:, :F] - h).abs()
     assert bool((d <= (2.0 ** -4 * h.abs() + 2.0 ** -10 * wide) * (1 + 2 * err) + 2 * err * h.abs()).all())
+
+
+@pytest.mark.parametrize("types", ["bf16", "f32"])
+def test_quantise_swiglu_of_far_gates(types):
+    """Gates whose exponentials leave float32's range: SiLU goes to 0 or to the gate; what is not finite is NaN."""
+    gates = torch.tensor([-1e38, -1e4, -200.0, -100.0, -89.0, -88.5, -60.0, 60.0, 100.0, 1e4, 0.0, -0.0, float("inf"),
+                          -float("inf"), float("nan"), 1.0]).to(TYPES[types])
+    x = torch.cat([gates, torch.full((16,), 2.0, dtype=gates.dtype)])[None].contiguous()
+    q, scale = pcm.pcm_swiglu_quant_fp8(gpu(x))
+    h = gates.double() * torch.sigmoid(gates.double()) * 2
+    fine = torch.isfinite(gates)
+    s = float(scale[0, 0])
+    assert abs(s - 2e4 / 448) <= 2.0 ** -7 * s          # 1e4 rounded to bf16
+    got = q[0].cpu().double()
+    assert bool(torch.isnan(got[~fine]).all())
+    assert bool(((got[fine] * s - h[fine]).abs() <= 2.0 ** -4 * h[fine].abs() * (1 + 2.0 ** -14) + 2.0 ** -10 * s).all())
 
 
 def quantised_weights(w):
