@@ -1063,13 +1063,14 @@ hipError_t allow_lds(K kernel, int bytes) {   // set on every launch (idempotent
 template <class E, class C, class CT, bool DX, class OUT, class OFF = uint32_t>
 hipError_t launch_rows(const GroupArgs& g, int window, hipStream_t s) {
     const int nt = (int)ceil_div(g.cols, C::BN);
-    const int64_t grid = ceil_div(most_row_tiles(g, C::BM) * nt, 8) * 8;
+    // (groups of few row tiles read their weights once for all of them in the other order)
+    const bool long_first = CT::BM < C::BM && g.offsets && mean_rows(g) >= 512 && expected_row_tiles(g, C::BM) * nt < 4 * 256;
+    // An eighth of the long tiles and one of the short ones, each rounded up, can be one more than an eighth of both.
+    const int64_t grid = ceil_div(most_row_tiles(g, C::BM) * nt, 8) * 8 + (long_first ? 8 : 0);
     if (grid >= int64_t(1) << 28) return hipErrorInvalidValue;   // counted in 32 bits
     const auto kernel = group_rows_kernel<E, C, CT, DX, OUT, OFF>;
     const hipError_t err = allow_lds(kernel, Slots<E, C>::BYTES);
     if (err != hipSuccess) return err;
-    // (groups of few row tiles read their weights once for all of them in the other order)
-    const bool long_first = g.offsets && mean_rows(g) >= 512 && expected_row_tiles(g, C::BM) * nt < 4 * 256;
     kernel<<<dim3((unsigned)grid), dim3(C::NT), Slots<E, C>::BYTES, s>>>(g, nt, window, long_first);
     return hipGetLastError();
 }

@@ -256,6 +256,16 @@ def test_tiles_forward_and_input_gradient(tile, length, types):
     close(dx, *rows64(c, c["dy"], c["w"], dx=True), length, "dx")
 
 
+@pytest.mark.parametrize("counts,cols", [([39 * 256 + 100], 1280), ([13 * 256 + 1, 12 * 256 + 128, 14 * 256 + 7], 1280),
+                                         ([20 * 256 + 5, 19 * 256], 1296), ([9 * 256 + 3] * 5, 1040)])
+def test_long_row_tiles_before_short_ones(counts, cols):
+    """Every tile is computed, also where neither the long tiles nor the short ones are a multiple of the XCDs."""
+    c = on(made((sum(counts), 1, counts, len(counts), 64, cols), torch.bfloat16, False, seed=cols))
+    y = torch.full((sum(counts), cols), float("nan"), dtype=torch.float32, device=DEV)
+    pcm.pcm_grouped_gemm(c["x"], c["w"], c["off"], y=y)
+    close(y, *rows64(c, c["x"], c["w"]), 64, "y")
+
+
 @pytest.mark.parametrize("gather", [True, False])
 @pytest.mark.parametrize("types", ["bf16-bf16", "bf16-f32", "f32-f32"])
 @pytest.mark.parametrize("N,K", [(1552, 1296), (848, 528), (80, 144)])
