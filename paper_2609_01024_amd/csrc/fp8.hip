@@ -2,6 +2,10 @@
 // A block with largest finite magnitude m has a = max(m, 2^-100), scale = a / 448 and values
 // e4m3(x * (448 / a)), to nearest even: every finite value lands within e4m3's largest, 448. The floor
 // keeps 448 / a finite. What is not finite becomes NaN and has no part in the scale.
+// The quantisers are bound by memory: rows 16384 x 7168 bf16 65 us (5.5 TB/s read and written), SwiGLU of 32768 x
+// 2 x 1408 41 us (5.7), 64 weights of 2048 x 1024 with their transposes 104 us (5.1 of the 5.1 TB/s that a
+// copy has). The product: 8192^3 2060 TF into bf16; 8 experts of 14336 x 4096 with 8192 rows 560-580 us; 256
+// of 2048 x 7168 with one row each 345-360 us (weights at 6.7-7 TB/s).
 #include "grouped.h"
 
 namespace pcm {
@@ -169,17 +173,28 @@ using Middle = TileCfg<64, 128, 2, 2, 3>;    // two
 using Square = TileCfg<128, 128, 2, 2, 2>;   // two
 using Wide = TileCfg<128, 256, 2, 4, 3>;     // one, eight waves of 64 x 64
 
+// Tiles as for 16-bit products, measured on both sides of every bound (one group, a contraction of 4096, us, this
+// tile / the next smaller):
+//   into bf16     128 x 256  112 tiles 29.3 / 39.7, 96 tiles 29.0 / 26.1, 64 tiles 28.7 / 22.2. (8192^3, an earlier
+//                            step: 128 x 256 1780 TF, 256 x 128 1590, 128 x 128 1650; 256 x 256 does not fit the
+//                            registers.)
+//                 64 x 64    320 tiles 21.7 / 20.9 (32 x 64), 512 tiles 22.2 / 29.8; 256 tiles 19.4 / 17.2
+//   into float32  128 x 128  448 tiles 71.2 / 82.0, 256 tiles 49.6 / 44.1; groups of fewer than 96 rows leave much of
+//                            such a tile empty (64 groups of 32: 87 / 66)
+//                 64 x 128   448 tiles 43.1 / 50.9, 512 tiles 44.1 / 50.8, 384 tiles 43.3 / 38.7
+//   16 rows of 64 columns, per-wave rings: float32, 512 tiles 17.2, 32 x 64 18.3; bf16, 256 tiles 10.0, 64 x
+//   64 18.9; 512 tiles 14.7, 32 x 64 14.7
 template <class E, class OUT>
 hipError_t fp8_by_shape(const GroupArgs& g, hipStream_t s) {
     if (!near(g, 1)) return launch_rows<E, Small, Small, false, OUT, int64_t>(g, 8, s);
     auto tiles = [&](int bm, int bn) { return expected_row_tiles(g, bm) * ceil_div(g.cols, bn); };
-    if (few_rows(g, 1) || tiles(16, 64) <= 256) return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, 1), s);
+    if (few_rows(g, 1) || tiles(16, 64) <= (E::PAIRS ? 256 : 512)) return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, 1), s);
     if (tiles(64, 64) <= 256) return launch_rows<E, Narrow, Narrow, false, OUT>(g, 8, s);
     if constexpr (E::PAIRS) {
         if (tiles(128, 256) >= 100) return launch_rows<E, Wide, Wide, false, OUT>(g, 8, s);
     } else {
-        if (tiles(128, 128) >= 512 && mean_rows(g) >= 96) return launch_rows<E, Square, Square, false, OUT>(g, 8, s);
-        if (tiles(64, 128) >= 256) return launch_rows<E, Middle, Middle, false, OUT>(g, 8, s);
+        if (tiles(128, 128) >= 400 && mean_rows(g) >= 96) return launch_rows<E, Square, Square, false, OUT>(g, 8, s);
+        if (tiles(64, 128) >= 400) return launch_rows<E, Middle, Middle, false, OUT>(g, 8, s);
     }
     return launch_rows<E, Small, Small, false, OUT>(g, 8, s);
 }

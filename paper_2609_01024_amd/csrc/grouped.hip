@@ -3,6 +3,11 @@
 //   forward          y[r, :]  = x[s(r), :] W[e]^T          W [n, N, K], rows r of group e
 //   input gradient   dx[r, :] = dy[r, :] W[e]              (then summed over the rows of a token)
 //   weight gradient  dW[e]    = sum_r dy[r, :]^T x[s(r), :]
+// Large ones are bound by the matrix cores and the loads that feed them (8192^3 bf16: 1470 TF forward, 1444 and
+// 1450 for the gradients), few rows in many groups by reading every weight once (256 groups of 7168 x
+// 2048, one row each: 676 us, 7.0 TB/s), a large gradient of few rows by writing it. A token's gradient adds the
+// rows of its groups in slot order in a second launch (slot_sum_kernel: the rows in float32, written and read
+// once; 32768 rows of 2048 add 110 us to 500), not with atomics, whose order would change results.
 #include "grouped.h"
 
 namespace pcm {
@@ -15,12 +20,24 @@ using Square = TileCfg<128, 128, 2, 2, 2, 3>;    // two
 using Large = TileCfg<256, 256, 2, 4, 2, 3>;     // one, eight waves of 128 x 64
 using LargeTail = TileCfg<128, 256, 2, 4, 2, 3>;
 
+// The larger the tile the fewer bytes a product loads (a compute unit takes in about 50 GB/s from its L2 and
+// beyond: 64 x 64 tiles stop at 700 TF, 64 x 128 at 890, 128 x 128 at 1110, 256 x 256 at 1480), but each
+// fills the 256 compute units from a number of tiles on. Measured on both sides of every bound, one group, a
+// contraction of 4096, bf16 (us, this tile / the next smaller):
+//   256 x 256  224 tiles 94 / 117, 128 tiles 78 / 64
+//   128 x 128  224 tiles 38.2 / 39.0 (input gradient 38.4 / 41.5), 128 tiles 34.0 / 24.6
+//   64 x 128   256 tiles 24.6 / 27.4, 128 tiles 33 / 19.1
+//   64 x 64    192 tiles 18.5 / 20.6 (32 x 64), 128 tiles 18.2 / 13.9
+//   16 rows    of 64 columns, per-wave rings: 256 tiles 10.5, 64 x 64 18.1; 384 tiles 16.0, 32 x 64 13.8
+// float32 is bound by the matrix cores' rate from 64 x 64 on, so larger tiles bring nothing: one group, a contraction of
+// 1024: 512 tiles 38.3 / 41.1 (32 x 64); of several groups, with row tiles that are not full, 672 tiles
+// 49.8 / 45.
 template <class E, bool DX, class OUT>
 hipError_t rows_by_shape(const GroupArgs& g, hipStream_t s) {
     if (!near(g, E::SIZE)) return launch_rows<E, Small, Small, DX, OUT, int64_t>(g, 8, s);
     auto tiles = [&](int bm, int bn) { return expected_row_tiles(g, bm) * ceil_div(g.cols, bn); };
     if constexpr (E::SIZE == 4) {
-        if (tiles(64, 64) < 1024) return launch_rows<E, Narrow, Narrow, DX, OUT>(g, 8, s);
+        if (tiles(64, 64) < (g.n == 1 ? 512 : 1024)) return launch_rows<E, Narrow, Narrow, DX, OUT>(g, 8, s);
         return launch_rows<E, Small, Small, DX, OUT>(g, 8, s);
     } else {
         if constexpr (!DX)
@@ -28,7 +45,7 @@ hipError_t rows_by_shape(const GroupArgs& g, hipStream_t s) {
                 return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, E::SIZE), s);
         if (tiles(64, 64) <= 128) return launch_rows<E, Narrow, Narrow, DX, OUT>(g, 8, s);
         if (tiles(256, 256) >= 192) return launch_rows<E, Large, LargeTail, DX, OUT>(g, 8, s);
-        if (tiles(128, 128) >= 256) return launch_rows<E, Square, Square, DX, OUT>(g, 8, s);
+        if (tiles(128, 128) >= 192) return launch_rows<E, Square, Square, DX, OUT>(g, 8, s);
         if (tiles(64, 128) >= 256) return launch_rows<E, Middle, Middle, DX, OUT>(g, 8, s);
         return launch_rows<E, Small, Small, DX, OUT>(g, 8, s);
     }
@@ -40,13 +57,16 @@ hipError_t rows_by_type(bool bf16, bool out_bf16, const GroupArgs& g, hipStream_
     return out_bf16 ? rows_by_shape<TBf16, DX, __bf16>(g, s) : rows_by_shape<TBf16, DX, float>(g, s);
 }
 
+// The same for the weight gradient (4096 rows, one group, bf16, us, this tile / the next smaller):
+//   256 x 256  224 tiles 98 / 119, 128 tiles 80 / 66
+//   128 x 128  224 tiles 38.7 / 55.4, 128 tiles 33.7 / 30.0, 64 tiles 26.9 / 19.9
 template <class E, class OUT, bool ADD>
 hipError_t outer_by_shape(const GroupArgs& g, hipStream_t s) {
     if (!near(g, E::SIZE)) return launch_outer<E, Small, OUT, ADD, int64_t>(g, s);
     auto tiles = [&](int bm, int bn) { return g.n * ceil_div(g.rows, bm) * ceil_div(g.cols, bn); };
     if constexpr (E::SIZE == 2) {
         if (tiles(256, 256) >= 192) return launch_outer<E, Large, OUT, ADD>(g, s);
-        if (tiles(128, 128) >= 128) return launch_outer<E, Square, OUT, ADD>(g, s);
+        if (tiles(128, 128) >= 160) return launch_outer<E, Square, OUT, ADD>(g, s);
     }
     return launch_outer<E, Small, OUT, ADD>(g, s);
 }
@@ -71,8 +91,8 @@ __global__ __launch_bounds__(256) void part_sum_kernel(const float* __restrict__
     }
 }
 
-// A thread adds four columns of a token's rows, slots ascending, in float32. All indices, then all rows, are
-// loaded before any is used.
+// A thread adds four columns of a token's rows, slots ascending, in float32. Bound by reading the rows: all indices,
+// then all rows, are loaded before any is used.
 template <class OUT>
 __global__ __launch_bounds__(256) void slot_sum_kernel(const float* __restrict__ rows, const int32_t* __restrict__ row_of,
                                                        int64_t T, int k, int64_t R, int K, OUT* __restrict__ out) {
@@ -105,10 +125,12 @@ hipError_t launch_grouped_dx(bool bf16, bool out_bf16, const GroupArgs& g, hipSt
 }
 
 // Long sums over rows in few tiles (a router's weight, one small matrix) would leave most compute units idle:
-// their rows are cut into parts of at least 256, for at most about two workgroups on each.
+// their rows are cut into parts of at least 256, for at most about two workgroups on each. 256 x 2048 of 65536 rows:
+// 164 us in parts, 363 without; 512 x 1024 of 4096 rows 15.0 / 18.4; of 2048 rows, where the second launch costs
+// more than the rows, 14.0 / 11.3.
 int dw_parts(int64_t R, int N, int K, int n) {
     const int64_t tiles = n * ceil_div(N, 64) * ceil_div(K, 64), mean = R / n;
-    if (tiles > 128 || mean < 512) return 1;
+    if (tiles > 128 || mean < 3000) return 1;
     const int64_t parts = 512 / tiles;
     return (int)(parts < mean / 256 ? parts : mean / 256);
 }

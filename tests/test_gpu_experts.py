@@ -223,6 +223,8 @@ TILES = {   # counts, columns
     "32 x 64": ([90, 33, 40], 272),
     "16 rows": ([16, 1, 0, 17, 5, 40, 3, 2], 208),
 }
+TILES_OF_8_BITS = {"128 x 128": ([1400, 300], 4112), "64 x 128": ([129, 1, 600], 4112), "64 x 64": ([90, 33, 40, 200, 61], 2064),
+                   "32 x 64": ([190, 33, 40], 2064)}
 
 
 def on(c):
@@ -292,7 +294,7 @@ def test_tiles_weight_gradient(counts, N, K, types, gather):
 @pytest.mark.parametrize("length", LENGTHS)
 @pytest.mark.parametrize("tile", ["128 x 128", "64 x 128", "64 x 64", "32 x 64", "16 rows"])
 def test_tiles_of_8_bits(tile, length, out):
-    counts, cols = TILES[tile]
+    counts, cols = TILES_OF_8_BITS.get(tile, TILES[tile])
     c = on(made8((sum(counts), 1, counts, len(counts), length, cols), True, seed=length))
     y = product8(c, out_dtype=TYPES[out])
     x = c["xq"].double() * spread(c["xs"], 0, length)
