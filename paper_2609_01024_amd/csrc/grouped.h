@@ -330,20 +330,32 @@ __device__ __forceinline__ void tile_loop(Side<E, C, C::BM, C::QA, A_KS, OFF>& A
                                           int64_t x_rows, const RowScales<C>* rs, ScalarPtr wsc) {
     using L = Slots<E, C>;
     static_assert(!GATHER || B_KS, "rows k are gathered");
-    constexpr int PA = C::QA, PB = C::QB, PER = PA + PB + (GATHER ? C::QB : 0);
+    // A gather's load covers GR rows k in turn. Two of them: their indices come by scalar loads, for the wait on a
+    // vector load drains the direct loads behind it (256 x 256 tiles: 64 groups of 2048 x 2048 664 -> 559 us,
+    // as without a gather); four or more: selecting costs more than that (128 x 128 26 -> 46, float32 164 -> 179).
+    constexpr int GR = GATHER ? 1024 / (C::BN * E::SIZE) : 1;
+    constexpr bool GS = GATHER && GR <= 2;
+    constexpr int PA = C::QA, PB = C::QB + (GATHER && !GS ? C::QB : 0), PER = PA + PB;
     // memory operations after those of slices kt + 1 when slice kt + NSA (A) and kt + NSB (B) are next
-    constexpr int LATER = (C::NSA - 2) * PER + (C::NSB > C::NSA ? PB + (GATHER ? C::QB : 0) : 0);
+    constexpr int LATER = (C::NSA - 2) * PER + (C::NSB > C::NSA ? PB : 0);
     static_assert(LATER <= 62, "vmcnt range");
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / C::WN, wn = wave % C::WN, kg = lane >> 4;
     const int KT = (len + E::KB - 1) / E::KB, rem = len - (KT - 1) * E::KB;   // slices; values of the last
     char* const ldsb = lds + L::B0;
-    int idx[C::QB];
-    auto index = [&](int q, int kt) { return gather[min(kt * E::KB + B.row(q, wave, lane), len - 1)]; };
+    typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+    int idx[C::QB][GS ? GR : 1];
+    auto index = [&](int q, int kt) {
+        if constexpr (GS)
+#pragma unroll
+            for (int j = 0; j < GR; ++j) idx[q][j] = ((ScalarInts)gather)[min(kt * E::KB + B.blk(q, wave) * GR + j, len - 1)];
+        else
+            idx[q][0] = gather[min(kt * E::KB + B.row(q, wave, lane), len - 1)];
+    };
     if constexpr (GATHER)
 #pragma unroll
-        for (int q = 0; q < C::QB; ++q) idx[q] = index(q, 0);
+        for (int q = 0; q < C::QB; ++q) index(q, 0);
     // One load of A's next slice into its slot (8-bit operands: the last one also the scales), or of B's.
     auto load_a = [&](int q, int slot, bool last) {
         char* S = lds + slot * L::SA;
@@ -354,9 +366,11 @@ __device__ __forceinline__ void tile_loop(Side<E, C, C::BM, C::QA, A_KS, OFF>& A
     auto load_b = [&](int q, int slot, bool last, int kt) {
         char* S = ldsb + slot * L::SB + B.blk(q, wave) * 1024;
         if constexpr (GATHER) {
-            const int64_t r = idx[q];
-            global_to_lds(B.base + (r < 0 ? 0 : r >= x_rows ? x_rows - 1 : r) * B.ld + B.off[0], S);
-            idx[q] = index(q, kt + 1);
+            int r = idx[q][0];
+            if constexpr (GS && GR == 2) r = lane >= 32 ? idx[q][1] : r;
+            r = min(max(r, 0), (int)x_rows - 1);
+            global_to_lds(B.base + (int64_t)r * B.ld + B.off[0], S);
+            index(q, kt + 1);
         } else {
             if (last) B.load_last(q, S, wave, lane, rem);
             else B.load(q, S);
@@ -394,7 +408,7 @@ __device__ __forceinline__ void tile_loop(Side<E, C, C::BM, C::QA, A_KS, OFF>& A
         if (s < KT) issue_b(s, is_last(s), s);
     }
     // slice 0 has landed: whatever was issued after it may be in flight
-    constexpr int AFTER0 = (C::NSA - 1) * PER + (C::NSB - C::NSA) * (PB + (GATHER ? C::QB : 0));
+    constexpr int AFTER0 = (C::NSA - 1) * PER + (C::NSB - C::NSA) * PB;
     if (KT >= C::NSB) __builtin_amdgcn_s_waitcnt(waitcnt_imm(AFTER0 <= 62 ? AFTER0 : 62, 0));
     else __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, 0));
     tile_barrier();
