@@ -882,7 +882,7 @@ __global__ __launch_bounds__(C::NT) void group_outer_kernel(GroupArgs g, int mt,
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Chunks of cm x cn tiles (about as many as an XCD's 32 compute units run at once, so that they share
     // operand tiles), dealt to the XCDs (workgroup id % 8) in turn, so that a group with many rows does not
-    // keep one of them busy alone (64 groups of very different size 1051 -> 852 us; contiguous eighths of the
+    // keep one of them busy alone (64 groups of very different size 1051 -> 852 us, now 720; contiguous eighths of the
     // tiles are 0-3% faster where all groups are alike; the groups sorted by rows first gave 769 us there
     // and cost 5-10% elsewhere, a search in front of every tile).
     const int slots = cm * cn, mc = (mt + cm - 1) / cm, nc = (nt + cn - 1) / cn;
