@@ -74,11 +74,12 @@ __device__ __forceinline__ uintx2 eight_e4m3(const Eight& x, float inv) {
 // SiLU(g) u in float32, near to correctly rounded: an error of some units in the last place would move as many
 // more codes across a border between two. bf16 inputs (this is what the kernel has time for next to its
 // memory traffic): e^-g = 2^i 2^f with i whole and f from one fused multiply-add (2^(-g log2 e) at once is off by
-// |g| units), and the hardware reciprocal (about 1 ulp); far below 0 the exponential is inf and the result
-// -0. float32 inputs: the library exponential and an IEEE division.
+// |g| units), and the hardware reciprocal (about 1 ulp). The exponent is bounded on both sides: past 2^31 the
+// product's rounding alone passes 128, and f would be no fraction. float32 inputs: the library exponential and an
+// IEEE division.
 __device__ __forceinline__ float gated(uint16_t, float g, float u) {
     constexpr float kLog2e = 1.44269504088896340736f;
-    const float c = fmaxf(g, -1000.0f), i = rintf(-c * kLog2e), f = fmaf(-c, kLog2e, -i);
+    const float c = fminf(fmaxf(g, -1000.0f), 1000.0f), i = rintf(-c * kLog2e), f = fmaf(-c, kLog2e, -i);
     return g * __builtin_amdgcn_rcpf(1.0f + ldexpf(__builtin_amdgcn_exp2f(f), (int)i)) * u;
 }
 __device__ __forceinline__ float gated(float, float g, float u) { return g / (1.0f + expf(-g)) * u; }

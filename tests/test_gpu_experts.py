@@ -554,6 +554,37 @@ def test_quantise_swiglu_of_far_gates(types):
     assert bool(((got[fine] * s - h[fine]).abs() <= 2.0 ** -4 * h[fine].abs() * (1 + 2.0 ** -14) + 2.0 ** -10 * s).all())
 
 
+def swiglu_alone(gates, up, types):
+    """(scale * 448, SiLU(gate) up in 64 bits, its bound) of gates that are alone in their blocks with one value of up:
+    the scale is the value itself. The bound is test_quantise_swiglu_rows' (from 110 on SiLU is the gate or 0), and, where its value lies
+    below the normal range, the gate times its exponential's spacing of 2^-149."""
+    x = torch.zeros((len(gates), 32), dtype=TYPES[types])
+    x[:, 0], x[:, 16] = gates, up
+    q, scale = pcm.pcm_swiglu_quant_fp8(gpu(x))
+    g = gates.double()
+    h = g * torch.sigmoid(g) * up
+    bound = (g.abs().clamp_max(110) + 8) * 2.0 ** -22 * h.abs() + g.abs().clamp_max(110) * 2.0 ** -149 * up
+    got = scale[:, 0].cpu().double() * 448
+    codes = q[:, 0].cpu().double() / 448
+    big = h.abs() >= 2.0 ** -90
+    assert torch.equal(codes[big], torch.sign(h[big]))     # the largest of its block
+    return got, h, bound
+
+
+def bf16_gates():
+    """Every finite bf16 value but the zeros."""
+    g = (torch.arange(65536, dtype=torch.int32) << 16).view(torch.float32)
+    return g[torch.isfinite(g) & (g != 0)]
+
+
+@pytest.mark.parametrize("types", ["bf16", "f32"])
+def test_quantise_swiglu_of_every_gate(types):
+    """SiLU of a large gate is the gate, however large, and of every other what it is."""
+    got, h, bound = swiglu_alone(bf16_gates(), 1.0, types)
+    bad = ~((got - h.abs().clamp_min(2.0 ** -100)).abs() <= bound + 2.0 ** -122)
+    assert not bad.any(), (int(bad.sum()), bf16_gates()[bad][:8].tolist())
+
+
 def quantised_weights(w):
     n, N, K = w.shape
     pad = torch.nn.functional.pad(w, (0, -K % 128, 0, -N % 128))
