@@ -556,8 +556,8 @@ def test_quantise_swiglu_of_far_gates(types):
 
 def swiglu_alone(gates, up, types):
     """(scale * 448, SiLU(gate) up in 64 bits, its bound) of gates that are alone in their blocks with one value of up:
-    the scale is the value itself. The bound is test_quantise_swiglu_rows' (from 110 on SiLU is the gate or 0), and, where its value lies
-    below the normal range, the gate times its exponential's spacing of 2^-149."""
+    the scale is the value itself. The bound is test_quantise_swiglu_rows' (from 110 on SiLU is the gate or 0) and the
+    gate times 2^-149, the spacing of an exponential below the normal range."""
     x = torch.zeros((len(gates), 32), dtype=TYPES[types])
     x[:, 0], x[:, 16] = gates, up
     q, scale = pcm.pcm_swiglu_quant_fp8(gpu(x))
@@ -583,6 +583,16 @@ def test_quantise_swiglu_of_every_gate(types):
     got, h, bound = swiglu_alone(bf16_gates(), 1.0, types)
     bad = ~((got - h.abs().clamp_min(2.0 ** -100)).abs() <= bound + 2.0 ** -122)
     assert not bad.any(), (int(bad.sum()), bf16_gates()[bad][:8].tolist())
+
+
+@pytest.mark.parametrize("types", ["bf16", "f32"])
+def test_quantise_swiglu_of_far_negative_gates(types):
+    """Large up values bring back SiLUs of gates whose exponentials, or their reciprocals, leave float32's range."""
+    gates = bf16_gates()
+    gates = gates[(gates < -1.0) & (gates > -100.0)]
+    got, h, bound = swiglu_alone(gates, 2.0 ** 100, types)
+    bad = ~((got - h.abs()).abs() <= bound)
+    assert not bad.any(), (int(bad.sum()), gates[bad][:16].tolist())
 
 
 def quantised_weights(w):
