@@ -332,8 +332,9 @@ pcm_status pcm_grouped_gemm(pcm_dtype dtype, pcm_dtype out_dtype, const void* x,
 
 /* Gradient by x of pcm_grouped_gemm. dy [R,N] and w [n,N,K] of `dtype`. row_of = NULL: dx [R,K],
  * dx[r, :] = dy[r, :] W[e] (T = R, k = 1). row_of [T,k] i32 (the rows that read each row of x, as in
- * pcm_paths; negative: none): dx [T,K], the sum of those rows' gradients, slots ascending, in float32,
- * rounded once; every row of dx is written. k is at most 8 and R at most T*k.
+ * pcm_paths; a number outside [offsets[0], offsets[n]), or [0, R) without offsets: none): dx [T,K], the
+ * sum of those rows' gradients, slots ascending, in float32, rounded once; every row of dx is written.
+ * k is at most 8 and R at most T*k.
  * ws: pcm_workspace_bytes(PCM_OP_GROUPED_DX, T, K, 0, n, k, dtype) bytes where row_of is given. */
 pcm_status pcm_grouped_gemm_dx(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* w,
                                const int32_t* offsets, const int32_t* row_of, int64_t T, int k,

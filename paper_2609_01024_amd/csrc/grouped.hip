@@ -92,25 +92,33 @@ __global__ __launch_bounds__(256) void part_sum_kernel(const float* __restrict__
     }
 }
 
-// A thread adds four columns of a token's rows, slots ascending, in float32. Bound by reading the rows: all indices,
-// then all rows, are loaded before any is used.
+// A thread adds four columns of a token's rows, slots ascending, in float32. Rows of no group are not added: the
+// product has not written them. Bound by reading the rows: all indices, then all rows, are loaded before any is
+// used.
 template <class OUT>
 __global__ __launch_bounds__(256) void slot_sum_kernel(const float* __restrict__ rows, const int32_t* __restrict__ row_of,
-                                                       int64_t T, int k, int64_t R, int K, OUT* __restrict__ out) {
+                                                       const int32_t* __restrict__ offsets, int n, int64_t T, int k,
+                                                       int64_t R, int K, OUT* __restrict__ out) {
+    int first = 0, count = (int)R;   // the groups' rows
+    if (offsets) {
+        first = offsets[0];
+        count = offsets[n] - first;
+        clamp_group((int)R, first, count);
+    }
     const int64_t per = K / 4, total = T * per;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t t = i / per, c = (i - t * per) * 4;
         int r[kMaxK];
         floatx4 v[kMaxK];
 #pragma unroll
-        for (int a = 0; a < kMaxK; ++a) r[a] = a < k && R > 0 ? row_of[t * k + a] : -1;
+        for (int a = 0; a < kMaxK; ++a) r[a] = a < k ? row_of[t * k + a] : -1;
 #pragma unroll
         for (int a = 0; a < kMaxK; ++a)
-            if (r[a] >= 0) v[a] = *(const floatx4*)(rows + min((int64_t)r[a], R - 1) * K + c);
+            if ((uint32_t)r[a] - (uint32_t)first < (uint32_t)count) v[a] = *(const floatx4*)(rows + (int64_t)r[a] * K + c);
         floatx4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int a = 0; a < kMaxK; ++a)
-            if (r[a] >= 0) sum += v[a];
+            if ((uint32_t)r[a] - (uint32_t)first < (uint32_t)count) sum += v[a];
         store4(out + t * K + c, sum);
     }
 }
@@ -155,12 +163,12 @@ hipError_t launch_grouped_dw(bool bf16, bool out_bf16, const GroupArgs& g, float
     return g.accumulate ? outer_by_shape<TBf16, float, true>(g, s) : outer_by_shape<TBf16, float, false>(g, s);
 }
 
-hipError_t launch_slot_sum(const float* rows, const int32_t* row_of, int64_t T, int k, int64_t R, int K, void* out,
-                           bool out_bf16, hipStream_t s) {
+hipError_t launch_slot_sum(const float* rows, const int32_t* row_of, const int32_t* offsets, int n, int64_t T, int k,
+                           int64_t R, int K, void* out, bool out_bf16, hipStream_t s) {
     const int64_t blocks = ceil_div(T * (K / 4), 256);
     const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)));
-    if (out_bf16) slot_sum_kernel<<<grid, dim3(256), 0, s>>>(rows, row_of, T, k, R, K, (__bf16*)out);
-    else slot_sum_kernel<<<grid, dim3(256), 0, s>>>(rows, row_of, T, k, R, K, (float*)out);
+    if (out_bf16) slot_sum_kernel<<<grid, dim3(256), 0, s>>>(rows, row_of, offsets, n, T, k, R, K, (__bf16*)out);
+    else slot_sum_kernel<<<grid, dim3(256), 0, s>>>(rows, row_of, offsets, n, T, k, R, K, (float*)out);
     return hipGetLastError();
 }
 

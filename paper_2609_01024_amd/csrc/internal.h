@@ -278,9 +278,9 @@ hipError_t launch_grouped_dx(bool bf16, bool out_bf16, const GroupArgs& g, hipSt
 hipError_t launch_grouped_dw(bool bf16, bool out_bf16, const GroupArgs& g, float* ws, hipStream_t s);
 int dw_parts(int64_t R, int N, int K, int n);
 hipError_t launch_grouped_fp8(bool out_bf16, const GroupArgs& g, hipStream_t s);
-// out[t, :] = sum over the slots a ascending of rows[row_of[t, a], :] (float32; negative indices: none).
-hipError_t launch_slot_sum(const float* rows, const int32_t* row_of, int64_t T, int k, int64_t R, int K, void* out,
-                           bool out_bf16, hipStream_t s);
+// out[t, :] = sum over the slots a ascending of rows[row_of[t, a], :] (float32; indices outside the groups' rows: none).
+hipError_t launch_slot_sum(const float* rows, const int32_t* row_of, const int32_t* offsets, int n, int64_t T, int k,
+                           int64_t R, int K, void* out, bool out_bf16, hipStream_t s);
 
 // 8-bit values with a scale for each block of 128 (fp8.hip). swiglu: x holds gate and up halves of 2 K.
 hipError_t launch_quant_rows(bool bf16, bool swiglu, const void* x, const int32_t* count, int64_t R, int K, uint8_t* q,

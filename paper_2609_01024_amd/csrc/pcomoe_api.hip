@@ -810,7 +810,7 @@ pcm_status pcm_grouped_gemm_dx(pcm_dtype dtype, pcm_dtype out_dtype, const void*
         if (err != hipSuccess) return PCM_ERR_HIP;
     }
     if (!row_of) return PCM_OK;
-    return from_hip(launch_slot_sum((const float*)ws, row_of, T, k, R, K, dx, out_dtype == PCM_BF16, s));
+    return from_hip(launch_slot_sum((const float*)ws, row_of, offsets, n, T, k, R, K, dx, out_dtype == PCM_BF16, s));
 }
 
 pcm_status pcm_grouped_gemm_dw(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const void* dy,

@@ -125,8 +125,8 @@ def pcm_grouped_gemm(x: torch.Tensor, w: torch.Tensor, offsets=None, row_token=N
 def pcm_grouped_gemm_dx(dy: torch.Tensor, w: torch.Tensor, offsets=None, row_of=None, dx=None,
                         out_dtype: Optional[torch.dtype] = None, ws: Optional[torch.Tensor] = None,
                         stream=None) -> torch.Tensor:
-    """The gradient by x: dy[r] w[e] for every row, or, with row_of [T, k] (negative: no row), its sum over
-    the rows of each token. ws: workspace_bytes(OP_GROUPED_DX, T, K, 0, n, k, dtype) bytes, with row_of."""
+    """The gradient by x: dy[r] w[e] for every row, or, with row_of [T, k] (outside the groups' rows: none),
+    its sum over the rows of each token. ws: workspace_bytes(OP_GROUPED_DX, T, K, 0, n, k, dtype) bytes, with row_of."""
     R, N = _matrix(dy, "dy")
     n, N_, K = _weights(w, offsets)
     _operand(dy, "dy")

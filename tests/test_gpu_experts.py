@@ -412,6 +412,32 @@ def test_input_gradient_of_tokens_without_rows():
     assert none.shape == (T, K) and bool((none == 0).all())
 
 
+@pytest.mark.parametrize("R,pad", [(10, 7), (40, 24)])
+@pytest.mark.parametrize("types", ["bf16", "f32"])
+def test_input_gradient_skips_rows_of_no_group(types, R, pad):
+    """Rows in front of offsets[0] and from offsets[n] on, and numbers that are no row, have no part in a
+    token's gradient: their workspace rows (NaN here) are not written."""
+    dt, k, n, K, N = TYPES[types], 4, 2, 48, 32
+    T = R + pad
+    g = torch.Generator().manual_seed(8)
+    off = torch.tensor([3, R // 2, R], dtype=torch.int32)          # of R + pad rows
+    of = torch.randint(-2, R + pad, (T, k), generator=g).int()
+    of[0] = torch.tensor([0, 2, R, R + pad - 1])                   # only rows of no group
+    of[1] = torch.tensor([3, R - 1, R + pad, 2 ** 31 - 1])
+    dy = torch.randn((R + pad, N), generator=g).to(dt)
+    dy[:3] = dy[R:] = float("nan")
+    w = torch.randn((n, N, K), generator=g).to(dt)
+    ws = torch.full((T * k * K * 4,), 0xFF, dtype=torch.uint8, device=DEV)
+    dx = pcm.pcm_grouped_gemm_dx(gpu(dy), gpu(w), gpu(off), gpu(of), out_dtype=torch.float32, ws=ws)
+    rows, mags = torch.zeros((R + pad, K), dtype=torch.float64), torch.zeros((R + pad, K), dtype=torch.float64)
+    for i, (a, b) in enumerate(((3, R // 2), (R // 2, R))):
+        rows[a:b] = dy[a:b].double() @ w[i].double()
+        mags[a:b] = dy[a:b].double().abs() @ w[i].double().abs()
+    take = lambda r: torch.where(((of >= 3) & (of < R))[:, :, None], r[of.clamp(0, R + pad - 1).long()], 0.0).sum(1)
+    close(dx, take(rows), take(mags), N + k, "dx")
+    assert bool((dx[0] == 0).all())
+
+
 def test_no_rows():
     w = torch.randn((3, 32, 48), device=DEV)
     off = torch.zeros(4, dtype=torch.int32, device=DEV)
