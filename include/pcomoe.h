@@ -321,7 +321,7 @@ pcm_status pcm_project_combine_scored(pcm_dtype dtype, const void* u, const void
  * offsets = NULL: one group (n = 1) of all R rows, row_token NULL: a plain product. R counts the rows of
  * the row buffers: rows from offsets[n] on are neither read nor written. Offsets are held inside [0, R]
  * and gathered indices inside [0, T), so no value of theirs reaches outside the buffers.
- * Limits: K and N multiples of 16; n <= 256; R and T below 2^30. Sums are float32. Deterministic. */
+ * Limits: K and N multiples of 16, at most 2^31 - 128; n <= 256; R and T below 2^30. Sums are float32. Deterministic. */
 
 /* y[r, :] = x[s(r), :] W[e]^T for the rows r of group e. x [T,K] and w [n,N,K] of `dtype` (PCM_F32 or
  * PCM_BF16), y [R,N] of out_dtype: PCM_F32, or for bf16 operands also PCM_BF16 (each float32 sum rounded

@@ -61,9 +61,11 @@ pcm_status check_paths(const pcm_paths* p) {
 
 // The experts' products: sizes, then types.
 constexpr int64_t kMaxGroupedRows = (int64_t)1 << 30;
+constexpr int kMaxGroupedWidth = INT32_MAX - 127;   // kernels count blocks as (width + 127) / 128
 pcm_status check_grouped(int64_t T, int64_t R, int K, int N, int n) {
     if (T < 0 || R < 0 || K < 1 || N < 1 || n < 1) return PCM_ERR_ARG;
-    if (K % 16 || N % 16 || n > kMaxN || T >= kMaxGroupedRows || R >= kMaxGroupedRows) return PCM_ERR_UNSUPPORTED;
+    if (K % 16 || N % 16 || K > kMaxGroupedWidth || N > kMaxGroupedWidth) return PCM_ERR_UNSUPPORTED;
+    if (n > kMaxN || T >= kMaxGroupedRows || R >= kMaxGroupedRows) return PCM_ERR_UNSUPPORTED;
     return PCM_OK;
 }
 bool plain_dtype(pcm_dtype d) { return d == PCM_F32 || d == PCM_BF16; }
@@ -178,7 +180,7 @@ const char* pcm_status_string(pcm_status s) {
     switch (s) {
         case PCM_OK: return "PCM_OK: success";
         case PCM_ERR_ARG: return "PCM_ERR_ARG: invalid argument (null or misaligned pointer, bad size, k > n)";
-        case PCM_ERR_UNSUPPORTED: return "PCM_ERR_UNSUPPORTED: outside the supported limits (k <= 8, n <= 256, H and F multiples of 64, T*k < 2^31; experts' products: K and N multiples of 16, T and R < 2^30)";
+        case PCM_ERR_UNSUPPORTED: return "PCM_ERR_UNSUPPORTED: outside the supported limits (k <= 8, n <= 256, H and F multiples of 64, T*k < 2^31; experts' products: K and N multiples of 16 up to 2^31 - 128, T and R < 2^30)";
         case PCM_ERR_WORKSPACE: return "PCM_ERR_WORKSPACE: workspace smaller than pcm_workspace_bytes()";
         case PCM_ERR_HIP: return "PCM_ERR_HIP: a HIP launch failed";
     }

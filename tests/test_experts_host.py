@@ -50,6 +50,24 @@ def test_sizes(L, name):
 
 
 @pytest.mark.parametrize("name", CALLS)
+def test_widths_near_32_bits(L, name):
+    """K and N whose number of blocks of 128 would pass 32 bits on the way are refused, the last one below is not."""
+    call, args = getattr(L, name), CALLS[name]
+    for width in ((1 << 31) - 112, (1 << 31) - 16):
+        assert call(*args(K=width)) == UNSUP, width
+        assert call(*args(N=width)) == UNSUP, width
+    assert call(*args(K=(1 << 31) - 128, N=(1 << 31) - 128, out=-1)) == ARG
+
+
+def test_quantiser_widths_near_32_bits(L):
+    for width in ((1 << 31) - 112, (1 << 31) - 16):
+        assert L.pcm_quant_fp8_rows(BF16, P, None, 1, width, P, P, None) == UNSUP
+        assert L.pcm_swiglu_quant_fp8(BF16, P, None, 1, width, P, P, None) == UNSUP
+        assert L.pcm_quant_fp8_weights(BF16, P, 1, width, 16, P, P, None, None, None) == UNSUP
+        assert L.pcm_quant_fp8_weights(BF16, P, 1, 16, width, P, P, None, None, None) == UNSUP
+
+
+@pytest.mark.parametrize("name", CALLS)
 def test_types(L, name):
     call, args = getattr(L, name), CALLS[name]
     assert call(*args(out=F16DOWN)) == ARG
