@@ -58,13 +58,25 @@ def _operand(t: torch.Tensor, what: str, dtype=None, shape=None, device: Optiona
         raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
 
 
+# The C entry points take widths and numbers of groups and slots in 32 bits; ctypes would cut larger ones.
+_INT_MAX = 2 ** 31 - 1
+
+
+def _too_wide(what: str):
+    raise ValueError(f"{what}: a size does not fit in 32 bits")
+
+
 def _weights(w: torch.Tensor, offsets: Optional[torch.Tensor]):
     """(n, N, K) of w [n, N, K], or of a plain product's w [N, K]."""
     if w.dim() == 2 and offsets is None:
-        return 1, w.shape[0], w.shape[1]
-    if w.dim() != 3:
+        n, (N, K) = 1, w.shape
+    elif w.dim() != 3:
         raise ValueError("w must have shape [n, N, K]")
-    return w.shape
+    else:
+        n, N, K = w.shape
+    if n > _INT_MAX or N > _INT_MAX or K > _INT_MAX:
+        _too_wide("w")
+    return n, N, K
 
 
 def _rows(x_rows: int, n: int, offsets, row_token, device) -> int:
@@ -84,6 +96,8 @@ def _rows(x_rows: int, n: int, offsets, row_token, device) -> int:
 def _matrix(t: torch.Tensor, what: str):
     if t.dim() != 2:
         raise ValueError(f"{what} must have two dimensions")
+    if t.shape[1] > _INT_MAX:
+        _too_wide(what)
     return t.shape
 
 
@@ -128,16 +142,16 @@ def pcm_grouped_gemm_dx(dy: torch.Tensor, w: torch.Tensor, offsets=None, row_of=
     """The gradient by x: dy[r] w[e] for every row, or, with row_of [T, k] (outside the groups' rows: none),
     its sum over the rows of each token. ws: workspace_bytes(OP_GROUPED_DX, T, K, 0, n, k, dtype) bytes, with row_of."""
     R, N = _matrix(dy, "dy")
-    n, N_, K = _weights(w, offsets)
+    n, _, K = _weights(w, offsets)
+    T, k = (R, 1) if row_of is None else _matrix(row_of, "row_of")
     _operand(dy, "dy")
     dev = dy.device
     _operand(w, "w", dy.dtype, (n, N, K) if w.dim() == 3 else (N, K), dev)
     _rows(R, n, offsets, None, dev)
     code = _code(dy.dtype)
     out = dx.dtype if dx is not None and out_dtype is None else out_dtype or dy.dtype
-    T, k, nbytes = R, 1, 0
+    nbytes = 0
     if row_of is not None:
-        T, k = _matrix(row_of, "row_of")
         _operand(row_of, "row_of", torch.int32, None, dev)
         nbytes = workspace_bytes(OP_GROUPED_DX, T, K, 0, n, k, code)
     ws = _workspace(ws, nbytes, dev, stream)
@@ -210,9 +224,11 @@ def pcm_quant_fp8_rows(x: torch.Tensor, count=None, q=None, scale=None, stream=N
 
 def pcm_swiglu_quant_fp8(gate_up: torch.Tensor, count=None, q=None, scale=None, stream=None):
     """pcm_quant_fp8_rows of SiLU(gate) * up; gate_up [R, 2F] holds a row's gate values before its up values."""
-    _, K2 = _matrix(gate_up, "gate_up")
-    if K2 % 2:
-        raise ValueError("gate_up must have an even number of columns")
+    if gate_up.dim() != 2 or gate_up.shape[1] % 2:
+        raise ValueError("gate_up must have two dimensions and an even number of columns")
+    K2 = gate_up.shape[1]
+    if K2 // 2 > _INT_MAX:
+        _too_wide("gate_up")
     return _quant_rows("pcm_swiglu_quant_fp8", gate_up, K2 // 2, count, q, scale, stream)
 
 
@@ -222,6 +238,8 @@ def pcm_quant_fp8_weights(w: torch.Tensor, transpose: bool = False, q=None, scal
     also (q_t, scale_t), the same codes and scales of every w^T (for the gradient by the input)."""
     if w.dim() not in (2, 3):
         raise ValueError("w must have shape [n, N, K] or [N, K]")
+    if max(w.shape) > _INT_MAX:
+        _too_wide("w")
     _operand(w, "w")
     dev, lead = w.device, tuple(w.shape[:-2])
     n, (N, K) = lead[0] if lead else 1, w.shape[-2:]

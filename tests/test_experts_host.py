@@ -170,6 +170,24 @@ def test_python_refuses_host_tensors():
             call()
 
 
+def test_python_refuses_sizes_past_32_bits():
+    """Sizes that the C entry points take in 32 bits are refused above them, not cut to what is left of them."""
+    wide, on = (1 << 32) + 64, dict(device="meta")
+    x, w = torch.empty((1, wide), **on), torch.empty((1, 64, wide), **on)
+    q, wq = torch.empty((1, wide), dtype=torch.float8_e4m3fn, **on), torch.empty((64, wide), dtype=torch.float8_e4m3fn, **on)
+    scale = torch.empty((1, wide // 128 + 1), **on)
+    for call in (lambda: pcm.pcm_grouped_gemm(x, w), lambda: pcm.pcm_grouped_gemm_dx(x, w.mT),
+                 lambda: pcm.pcm_grouped_gemm_dx(torch.empty((1, 64), **on), w),
+                 lambda: pcm.pcm_grouped_gemm_dx(torch.empty((1, 64), **on), w[:, :, :64], row_of=x.int()),
+                 lambda: pcm.pcm_grouped_gemm_dw(x, torch.empty((1, 64), **on)),
+                 lambda: pcm.pcm_grouped_gemm_dw(torch.empty((1, 64), **on), x),
+                 lambda: pcm.pcm_quant_fp8_rows(x), lambda: pcm.pcm_swiglu_quant_fp8(torch.empty((1, 2 * wide), **on)),
+                 lambda: pcm.pcm_quant_fp8_weights(w), lambda: pcm.pcm_quant_fp8_weights(w.mT),
+                 lambda: pcm.pcm_grouped_gemm_fp8(q, scale, wq, scale)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+
+
 def test_python_refuses_shapes():
     x = torch.zeros(4, 64)
     with pytest.raises(ValueError):
