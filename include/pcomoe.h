@@ -375,8 +375,12 @@ pcm_status pcm_quant_fp8_weights(pcm_dtype dtype, const void* w, int n, int N, i
 
 /* pcm_grouped_gemm of 8-bit operands: y[r, c] = sum over the blocks b of K of
  * x_scale[s(r), b] w_scale[e, c / 128, b] sum over k in b of x[s(r), k] w[e, c, k].
- * x [T,K] u8 with x_scale [T, ceil(K/128)], w [n,N,K] u8 with w_scale [n, ceil(N/128), ceil(K/128)] (any
- * float32 scales), y [R,N] of out_dtype. The scaled blocks are added in float32. PCM_F32: so are a block's
+ * x [T,K] u8 with x_scale [T, ceil(K/128)], w [n,N,K] u8 with w_scale [n, ceil(N/128), ceil(K/128)], y [R,N]
+ * of out_dtype. A block's two scales are multiplied with each other first, in float32, then with its sum. Their
+ * product has to be a normal float32 number (2^-126 up to below 2^128): a smaller one loses bits and from 2^-150
+ * down the whole block, a larger one is infinite, which makes NaN of a block that adds up to 0. (Quantised blocks
+ * keep to it where their largest magnitudes multiply to 2^-108 at least and below 2^128.)
+ * The scaled blocks are added in float32. PCM_F32: so are a block's
  * products (as bf16 values, exactly, at half the rate). PCM_BF16: on the 8-bit matrix cores, which cut
  * products below 2^-13 of the largest among their neighbours (1.3e-5 of the result's norm on normal
  * values; the rounding to bf16 is 1.7e-3).

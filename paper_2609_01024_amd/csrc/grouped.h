@@ -300,7 +300,7 @@ struct Step {
 #pragma unroll
             for (int mb = 0; mb < C::MB; ++mb) {
                 av[mb] = E::value(a[mb]);
-                f[mb] = scale[mb] * ws;
+                f[mb] = scale[mb] * ws;   // (one product a row; scaling the sums twice would double what stands beside an MFMA)
             }
 #pragma unroll
             for (int nb = 0; nb < C::NBK; ++nb) {

@@ -680,6 +680,32 @@ def test_product_of_8_bits(shape, out, gather):
     close(product8(c, out_dtype=TYPES[out]), forward64(c, x, w), forward64(c, x.abs(), w.abs()), c["K"], "y", EIGHT[out])
 
 
+# contraction 272: three blocks of codes; row tiles of 16, 32 and 64 or 128 rows (kernels with and without pairs)
+SCALE_SHAPES = {"16 rows": ([16, 1, 0, 17, 5], 208), "32 x 64": ([190, 33, 40], 2064), "large": ([1400, 300], 4112)}
+
+
+@pytest.mark.parametrize("x_exp,w_exp", [(-60, -66), (-109, -17), (0, -126), (60, 45), (118, -14), (-20, 125)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SCALE_SHAPES)
+def test_product_of_8_bits_at_the_ends_of_the_scales(shape, out, x_exp, w_exp):
+    """Products of scales from the smallest normal number to as large as leaves the results finite, and blocks of
+    zeros under them, which count as nothing."""
+    counts, cols = SCALE_SHAPES[shape]
+    c = made8((sum(counts), 1, counts, len(counts), 272, cols), True, seed=3)
+    one_up = torch.randint(0, 2, c["xs"].shape, generator=torch.Generator().manual_seed(1))
+    c["xs"] = torch.exp2((one_up + x_exp).float())
+    c["ws"] = torch.full_like(c["ws"], 2.0 ** w_exp)
+    c["xq"].view(torch.uint8)[:, 128:256] = 0
+    c["xq"].view(torch.uint8)[::5] = 0
+    c = on(c)
+    y = product8(c, out_dtype=TYPES[out])
+    x = c["xq"].double() * spread(c["xs"], 0, 272)
+    want, mag = rows64(c, x[c["tok"].long()], c["wq"].double() * 2.0 ** w_exp)
+    assert float(mag.max()) < 2.0 ** 127
+    close(y, want, mag, 272, "y", EIGHT[out])
+    assert bool((y[(c["tok"] % 5) == 0] == 0).all())
+
+
 def test_product_of_8_bits_without_offsets():
     c = made8((50, 1, None, 1, 400, 144), False)
     x, w = dequantised(c)
