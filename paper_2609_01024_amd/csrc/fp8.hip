@@ -199,7 +199,7 @@ template <class E, class OUT>
 hipError_t fp8_by_shape(const GroupArgs& g, hipStream_t s) {
     if (!near(g, 1)) return launch_rows<E, Small, Small, false, OUT, int64_t>(g, 8, s);
     auto tiles = [&](int bm, int bn) { return expected_row_tiles(g, bm) * ceil_div(g.cols, bn); };
-    if (few_rows(g, 1) || tiles(16, 64) <= (E::PAIRS ? 256 : 512)) return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, 1), s);
+    if (few_rows(g, 1) || tiles(16, 64) <= (E::PAIRS ? 256 : 512)) return launch_thin<E, OUT>(g, 8, weights_once(g, 1), s);
     if (tiles(64, 64) <= 256) return launch_rows<E, Narrow, Narrow, false, OUT>(g, 8, s);
     if constexpr (E::PAIRS) {
         if (tiles(128, 256) >= 100) return launch_rows<E, Wide, Wide, false, OUT>(g, 8, s);

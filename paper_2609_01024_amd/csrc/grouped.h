@@ -928,21 +928,23 @@ __global__ __launch_bounds__(C::NT) void group_outer_kernel(GroupArgs g, int mt,
 }
 
 // Few rows a group: the weights are what there is to read, so a compute unit has to keep many of their
-// bytes in flight. A workgroup takes BM (16 or 32) rows and 64 columns, and each of its NW waves its own
-// slices of the contraction (every NW-th) through a ring of its own, with no barrier until the waves' sums
+// bytes in flight. A workgroup takes 16 rows and 64 columns, and each of its four waves its own
+// slices of the contraction (every fourth) through a ring of its own, with no barrier until the waves' sums
 // are added, in order, at the end.
-template <class E, int BM, int NW, int NS>
+template <class E>
 struct ThinCfg {
+    static constexpr int BM = 16, NW = 4, NS = 2;   // rows, waves, slices of a ring
     using C = TileCfg<BM, 64, 1, 1, 2>;   // the layout of one wave
     static constexpr int SLOT = (BM + 64) * 128 + (E::SCALED ? 256 : 0), WAVE = NS * SLOT;
     static constexpr int BYTES = NW * WAVE, PER = C::QA + C::QB + (E::SCALED ? 1 : 0);
     static_assert(NW == C::NBK, "each wave adds one block of columns");
     static_assert(BYTES <= 160 * 1024 && (NS - 1) * PER <= 62 && BM * 256 <= WAVE, "LDS, vmcnt range, sums");
 };
-template <class E, int BM, int NW, int NS, class OUT>
-__global__ __launch_bounds__(NW * 64) void group_thin_kernel(GroupArgs g, int nt, int window, bool once) {
-    using T = ThinCfg<E, BM, NW, NS>;
+template <class E, class OUT>
+__global__ __launch_bounds__(ThinCfg<E>::NW * 64) void group_thin_kernel(GroupArgs g, int nt, int window, bool once) {
+    using T = ThinCfg<E>;
     using C = typename T::C;
+    constexpr int BM = T::BM, NW = T::NW, NS = T::NS;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     int* const s_item = (int*)lds;
     if (!group_item<BM>(g, nt, window, s_item)) return;   // workgroup-uniform
@@ -1089,17 +1091,16 @@ hipError_t launch_rows(const GroupArgs& g, int window, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <class E, int BM, int NS, class OUT>
+template <class E, class OUT>
 hipError_t launch_thin(const GroupArgs& g, int window, bool once, hipStream_t s) {
-    constexpr int NW = 4;
+    using T = ThinCfg<E>;
     const int nt = (int)ceil_div(g.cols, 64);
-    const int64_t grid = ceil_div(most_row_tiles(g, BM) * nt, 8) * 8;
+    const int64_t grid = ceil_div(most_row_tiles(g, T::BM) * nt, 8) * 8;
     if (grid >= int64_t(1) << 28) return hipErrorInvalidValue;
-    const auto kernel = group_thin_kernel<E, BM, NW, NS, OUT>;
-    constexpr int bytes = ThinCfg<E, BM, NW, NS>::BYTES;
-    const hipError_t err = allow_lds(kernel, bytes);
+    const auto kernel = group_thin_kernel<E, OUT>;
+    const hipError_t err = allow_lds(kernel, T::BYTES);
     if (err != hipSuccess) return err;
-    kernel<<<dim3((unsigned)grid), dim3(NW * 64), bytes, s>>>(g, nt, window, once);
+    kernel<<<dim3((unsigned)grid), dim3(T::NW * 64), T::BYTES, s>>>(g, nt, window, once);
     return hipGetLastError();
 }
 

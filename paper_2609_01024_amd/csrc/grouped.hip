@@ -42,7 +42,7 @@ hipError_t rows_by_shape(const GroupArgs& g, hipStream_t s) {
     } else {
         if constexpr (!DX)
             if (few_rows(g, E::SIZE) || tiles(16, 64) <= 256)
-                return launch_thin<E, 16, 2, OUT>(g, 8, weights_once(g, E::SIZE), s);
+                return launch_thin<E, OUT>(g, 8, weights_once(g, E::SIZE), s);
         if (tiles(64, 64) <= 128) return launch_rows<E, Narrow, Narrow, DX, OUT>(g, 8, s);
         if (tiles(256, 256) >= 192) return launch_rows<E, Large, LargeTail, DX, OUT>(g, 8, s);
         if (tiles(128, 128) >= 192) return launch_rows<E, Square, Square, DX, OUT>(g, 8, s);
