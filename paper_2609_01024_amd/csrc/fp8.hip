@@ -188,7 +188,9 @@ using Wide = TileCfg<128, 256, 2, 4, 3>;     // one, eight waves of 64 x 64
 // tile / the next smaller):
 //   into bf16     128 x 256  112 tiles 29.3 / 39.7, 96 tiles 29.0 / 26.1, 64 tiles 28.7 / 22.2. (8192^3, an earlier
 //                            step: 128 x 256 1780 TF, 256 x 128 1590, 128 x 128 1650; 256 x 256 does not fit the
-//                            registers.)
+//                            registers.) Many groups of few rows do not need a bound of their own (4096 columns, a
+//                            contraction of 2048, this / 64 x 64): 64 groups of 17 rows 109 / 108, 32 114 / 113, 64
+//                            122 / 146, 96 128 / 172; 128 groups of 32 218 / 220, 48 223 / 231
 //                 64 x 64    320 tiles 21.7 / 20.9 (32 x 64), 512 tiles 22.2 / 29.8; 256 tiles 19.4 / 17.2
 //   into float32  128 x 128  448 tiles 71.2 / 82.0, 256 tiles 49.6 / 44.1; groups of fewer than 96 rows leave much of
 //                            such a tile empty (64 groups of 32: 87 / 66)
@@ -199,7 +201,7 @@ template <class E, class OUT>
 hipError_t fp8_by_shape(const GroupArgs& g, hipStream_t s) {
     if (!near(g, 1)) return launch_rows<E, Small, Small, false, OUT, int64_t>(g, 8, s);
     auto tiles = [&](int bm, int bn) { return expected_row_tiles(g, bm) * ceil_div(g.cols, bn); };
-    if (few_rows(g, 1) || tiles(16, 64) <= (E::PAIRS ? 256 : 512)) return launch_thin<E, OUT>(g, 8, weights_once(g, 1), s);
+    if (few_rows(g, 1, E::PAIRS ? 14 : 16) || tiles(16, 64) <= (E::PAIRS ? 256 : 512)) return launch_thin<E, OUT>(g, 8, weights_once(g, 1), s);
     if (tiles(64, 64) <= 256) return launch_rows<E, Narrow, Narrow, false, OUT>(g, 8, s);
     if constexpr (E::PAIRS) {
         if (tiles(128, 256) >= 100) return launch_rows<E, Wide, Wide, false, OUT>(g, 8, s);

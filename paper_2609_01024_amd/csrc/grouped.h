@@ -713,7 +713,11 @@ __device__ bool group_item(const GroupArgs& g, int nt, int window, int* s_item) 
 // The same with each XCD's eighth of the row tiles of more than TBM rows before its eighth of the shorter ones,
 // which then fill the last round instead of lengthening it: for products of few rounds (Mixtral-shaped down
 // projection, 576 tiles: 954 -> 847 us; with more rounds, or a row tile or two a group, the order above shares
-// operands better: 256 rows each in 64 groups 176 -> 212 us).
+// operands better: 256 rows each in 64 groups 176 -> 212 us). Both sides of launch_rows' bounds (a contraction of 4096,
+// 8 to 32 groups, us, this order / the one above): a mean of 256 rows, 384 tiles 207-210 / 206-207, 768 tiles 348-358 /
+// 332-340; of 400, 528 tiles 228-238 / 219-222; of 512, 320 tiles 156-171 / 177-199, 640 tiles 286-299 / 290-305, 1280
+// tiles 550-585 / 522-550; of 700, 400 to 1650 tiles within 2% of each other; of 1000, 560 tiles 245-266 / 269-299. (Past
+// the bound of 1024 tiles a mean of 1000 and more would still gain: 1120 tiles 457-468 / 469-489.)
 template <int BM, int TBM>
 __device__ bool group_item_long_first(const GroupArgs& g, int nt, int window, int* s_item) {
     if (threadIdx.x < 64) {
@@ -782,10 +786,17 @@ inline int64_t mean_rows(const GroupArgs& g) {
 // Whether a mean of few rows a group makes the per-wave rings faster than 64 x 64 tiles and more: enough slices of
 // 128 bytes of the contraction for the rings to run (64 groups, 4096 columns: bf16 54 against 56 us at 8
 // slices, 38 against 31 at 4; 8 bits, mean of 8 rows: 110 against 108 us at 16, 78 against 64 at 8; a mean of 16 rows
-// needs twice as many, the second row tile of some groups reading the weights again).
-inline bool few_rows(const GroupArgs& g, int64_t size) {
+// needs twice as many, the second row tile of some groups reading the weights again). The bound of the mean, 16, and 14
+// where 8-bit values make results in bf16, whose tiles are the faster ones: random counts, 2048 columns, a contraction
+// of 7168, rings / tiles, us: 256 groups, 8 bits into bf16, mean of 12 622 / 666, 14 679 / 677, 16 755 / 677; into
+// float32 14 695 / 747, 16 759 / 751; bf16 12 1097 / 1220, 16 1210 / 1223; 64 groups, 8 bits into bf16 12 166 / 171, 16
+// 198 / 172, into float32 14 190 / 187, 16 204 / 188, bf16 14 302 / 311, 16 314 / 311. (A contraction of 4096 in 64
+// groups is the one found where bf16 results of a mean of 16 would keep the rings: 120 / 131; 256 groups 450 / 399.)
+// The counts are the device's, the host has their mean only: where nine tenths of the rows lie in one group, rings take
+// up to 1.4 times the tiles' time (256 groups of 2048 x 2048, bf16, mean of 16 453 / 349, of 8 298 / 253).
+inline bool few_rows(const GroupArgs& g, int64_t size, int most = 16) {
     const int64_t mean = mean_rows(g);
-    return mean <= 16 && ceil_div(g.len * size, 128) >= (size == 1 ? 2 : 1) * (mean > 8 ? 16 : 8);
+    return mean <= most && ceil_div(g.len * size, 128) >= (size == 1 ? 2 : 1) * (mean > 8 ? 16 : 8);
 }
 // Whether the weights are worth reading non-temporally by groups of one row tile, which read them once:
 // together they are more than half of the 256 MB MALL.

@@ -29,9 +29,13 @@ using LargeTail = TileCfg<128, 256, 2, 4, 2, 3>;
 //   64 x 128   256 tiles 24.6 / 27.4, 128 tiles 33 / 19.1
 //   64 x 64    192 tiles 18.5 / 20.6 (32 x 64), 128 tiles 18.2 / 13.9
 //   16 rows    of 64 columns, per-wave rings: 256 tiles 10.5, 64 x 64 18.1; 384 tiles 16.0, 32 x 64 13.8
-// float32 is bound by the matrix cores' rate from 64 x 64 on, so larger tiles bring nothing: one group, a contraction of
-// 1024: 512 tiles 38.3 / 41.1 (32 x 64); of several groups, with row tiles that are not full, 672 tiles
-// 49.8 / 45.
+// float32: 64 x 64 / 32 x 64, 1024 columns, a contraction of 1024. Each step of a few hundred tiles is a round of
+// workgroups, in which now the one and now the other is ahead; the bounds are where neither is by much on both sides:
+//   one group         384 tiles 38.6 / 31.5, 448 38.4 / 41.3, 512 38.8 / 41.2, 640 53.6 / 49.0, 768 54.4 / 57.6, 2048 135 / 145
+//   8 and 16 groups   368 tiles 38.1 / 30.6, 496 38.5 / 41.0, 560-624 53.4 / 48.3, 752 54.2 / 56.9, 1008 71.5 / 74.4, 2032 135 / 145
+//   64 groups (row tiles that are not full)   752 tiles 82 / 64, 1008 82 / 72, 1264 84 / 90, 1520 123 / 106, 2032 147 / 135
+// 64 x 64 reaches 128 TF in 2048 tiles. 128 x 128 would bring 4% to one large group (8192 x 4096 x 4096 1964 / 2043) and
+// cost 13% in 8 groups of 1024 rows (624 / 552), 64 x 128 1% and 5%; the input gradient's layout has no such tiles.
 template <class E, bool DX, class OUT>
 hipError_t rows_by_shape(const GroupArgs& g, hipStream_t s) {
     if (!near(g, E::SIZE)) return launch_rows<E, Small, Small, DX, OUT, int64_t>(g, 8, s);
@@ -135,8 +139,10 @@ hipError_t launch_grouped_dx(bool bf16, bool out_bf16, const GroupArgs& g, hipSt
 
 // Long sums over rows in few tiles (a router's weight, one small matrix) would leave most compute units idle:
 // their rows are cut into parts of at least 256, for at most about two workgroups on each. 256 x 2048 of 65536 rows:
-// 164 us in parts, 363 without; 512 x 1024 of 4096 rows 15.0 / 18.4; of 2048 rows, where the second launch costs
-// more than the rows, 14.0 / 11.3.
+// 164 us in parts, 363 without. Both sides of the bounds (in parts / without): 128 tiles 4096 rows 15.9 / 19.6, 2600
+// rows 14.7 / 14.4, 2048 rows, where the second launch costs more than the rows, 14.6 / 12.2; 64 tiles 2600 rows 13.9
+// / 15.1, 2048 rows 13.7 / 12.8; 160 tiles 4096 rows 21.2 / 21.2, 8192 rows 33.9 / 37.2; 256 tiles 4096 rows 23.6
+// / 20.9, 16384 rows 68.3 / 67.2.
 int dw_parts(int64_t R, int N, int K, int n) {
     const int64_t tiles = n * ceil_div(N, 64) * ceil_div(K, 64), mean = R / n;
     if (tiles > 128 || mean < 3000) return 1;
