@@ -5,7 +5,8 @@ As in binding.py the functions carry the C entry points' names, check and marsha
 allocate what the caller does not pass. Rows and groups are a PathTable's: offsets [n+1] int32 (its
 expert_offsets), row_token [R] int32 (row of x behind each row) and row_of [T, k] int32. Without offsets
 there is one group and w may be [N, K]. Tensors must be contiguous, on the current device; 8-bit values
-are torch.float8_e4m3fn, their scales float32."""
+are torch.float8_e4m3fn, their scales float32. Autograd does not record these calls, whatever their inputs
+require: a backward pass makes the gradients' calls itself."""
 from __future__ import annotations
 
 from typing import Optional
