@@ -438,6 +438,20 @@ def test_input_gradient_skips_rows_of_no_group(types, R, pad):
     assert bool((dx[0] == 0).all())
 
 
+def test_input_gradient_of_one_group_skips_numbers_that_are_no_row():
+    """The same without offsets: the rows are [0, R)."""
+    T, k, R, K, N = 7, 3, 12, 64, 48
+    g = torch.Generator().manual_seed(9)
+    of = torch.randint(-3, R + 4, (T, k), generator=g).int()
+    of[2] = torch.tensor([R, -1, 2 ** 31 - 1])
+    dy, w = torch.randn((R, N), generator=g), torch.randn((N, K), generator=g)
+    ws = torch.full((T * k * K * 4,), 0xFF, dtype=torch.uint8, device=DEV)
+    dx = pcm.pcm_grouped_gemm_dx(gpu(dy), gpu(w), row_of=gpu(of), ws=ws)
+    take = lambda r: torch.where(((of >= 0) & (of < R))[:, :, None], r[of.clamp(0, R - 1).long()], 0.0).sum(1)
+    close(dx, take(dy.double() @ w.double()), take(dy.double().abs() @ w.double().abs()), N + k, "dx")
+    assert bool((dx[2] == 0).all())
+
+
 def test_no_rows():
     w = torch.randn((3, 32, 48), device=DEV)
     off = torch.zeros(4, dtype=torch.int32, device=DEV)
