@@ -92,7 +92,8 @@ typedef enum pcm_op {
     PCM_OP_ROUTE_LOGITS = 6,
     PCM_OP_ROUTE_PATHS = 7,
     PCM_OP_GROUPED_DX = 8,
-    PCM_OP_GROUPED_DW = 9
+    PCM_OP_GROUPED_DW = 9,
+    PCM_OP_GRAD_NORM = 10
 } pcm_op;
 
 /* Path table and grouped dispatch layout of T tokens (caller-owned device buffers).
@@ -390,6 +391,105 @@ pcm_status pcm_grouped_gemm_fp8(pcm_dtype out_dtype, const uint8_t* x, const flo
                                 const uint8_t* w, const float* w_scale, const int32_t* offsets,
                                 const int32_t* row_token, int64_t T, int64_t R, int K, int N, int n,
                                 void* y, void* stream);
+
+/* ---------------------------------------------------------------- training around the experts' products
+ * What a training step does between the products above, with its gradients. `dtype` is that of the inputs,
+ * `out_dtype` that of the result, each PCM_F32 or PCM_BF16; computed in float32, rounded once, to nearest even.
+ * Limits: widths (H, F) multiples of 16, at most 2^31 - 128; k <= 8; n <= 256; T and R below 2^30. Outputs must not
+ * overlap inputs (but for the gradients clipped in place). Deterministic. */
+
+/* Rows of tokens. row_of [T,k] i32: the row of pair (t, a), as in pcm_paths; a number outside [offsets[0],
+ * offsets[n]) (offsets [n+1] i32, which may be a part of a table's: a rank that holds some of the experts), or
+ * [0, R) without offsets (then n = 1), is no row and has no part. No two pairs have the same row. R counts the rows
+ * of the row buffers. weights [T,k] f32, or NULL: 1.
+ *
+ * Tokens to rows: y[r, :] = weights[t, a] x[t, :] for r = row_of[t, a]. x [T,H], y [R,H]; rows of no pair are left
+ * as they were. */
+pcm_status pcm_dispatch_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const int32_t* row_of,
+                             const float* weights, const int32_t* offsets, int64_t T, int k, int64_t R,
+                             int H, int n, void* y, void* stream);
+
+/* Its gradients: dx[t, :] = sum over a (ascending) of weights[t, a] dy[r, :], every row written; dweights[t, a] =
+ * sum over the columns of dy[r, :] x[t, :], 0 for a pair without a row. dy [R,H] and x [T,H] of `dtype`, dx [T,H] of
+ * out_dtype, dweights [T,k] f32. dx or dweights may be NULL: not wanted; x may be NULL without dweights. */
+pcm_status pcm_dispatch_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* x,
+                                  const int32_t* row_of, const float* weights, const int32_t* offsets,
+                                  int64_t T, int k, int64_t R, int H, int n, void* dx, float* dweights,
+                                  void* stream);
+
+/* Rows back to tokens: y[t, :] = [y[t, :] +] sum over a (ascending) of weights[t, a] o[r, :], every row written.
+ * o [R,H], y [T,H]. accumulate adds into y (PCM_F32 only). */
+pcm_status pcm_combine_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* o, const int32_t* row_of,
+                            const float* weights, const int32_t* offsets, int64_t T, int k, int64_t R,
+                            int H, int n, void* y, int accumulate, void* stream);
+
+/* Its gradients: d_o[r, :] = weights[t, a] dy[t, :], rows of no pair left as they were; dweights[t, a] = sum over
+ * the columns of o[r, :] dy[t, :], 0 for a pair without a row. dy [T,H] and o [R,H] of `dtype`, d_o [R,H] of
+ * out_dtype, dweights [T,k] f32. d_o or dweights may be NULL: not wanted; o may be NULL without dweights. */
+pcm_status pcm_combine_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* o,
+                                 const int32_t* row_of, const float* weights, const int32_t* offsets,
+                                 int64_t T, int k, int64_t R, int H, int n, void* d_o, float* dweights,
+                                 void* stream);
+
+/* SwiGLU between the experts' products: u[r, :] = SiLU(gate) * up. gate_up [R, 2F], a row's gate values before its up
+ * values; u [R,F]. count: as for pcm_swiglu_quant_fp8, which quantises the same values. */
+pcm_status pcm_swiglu(pcm_dtype dtype, pcm_dtype out_dtype, const void* gate_up, const int32_t* count,
+                      int64_t R, int F, void* u, void* stream);
+
+/* Its gradient by gate_up, from it and du [R,F] (both of `dtype`): dgate_up [R, 2F] of out_dtype, in the same order,
+ * dgate = du up s (1 + gate (1 - s)), dup = du gate s, s = 1 / (1 + exp(-gate)). du * up is formed first. */
+pcm_status pcm_swiglu_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* gate_up, const void* du,
+                           const int32_t* count, int64_t R, int F, void* dgate_up, void* stream);
+
+/* The mix along each token's paths: z[tgt_row_of[t, b], :] = sum over a (ascending) of beta[t, a, b] u[src_row_of[t, a],
+ * :] over the paths (a, b) of path_bits [T] (bit a*k+b). beta [T,k,k] f32; src_row_of and tgt_row_of [T,k] i32: row_of
+ * of a pcm_paths for both, src_row_of and tgt_row_of of a pcm_scored_paths. u [R_src,F], z [R_tgt,F]. A number that is no
+ * row ([0, R_src), [0, R_tgt)) has no part; no two pairs have the same row of a buffer. A target without paths has
+ * zeros; rows of no pair are left as they were. beta where there is no path and its source's row are not used. */
+pcm_status pcm_mix_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* u, const uint64_t* path_bits,
+                        const float* beta, const int32_t* src_row_of, const int32_t* tgt_row_of, int64_t T,
+                        int k, int64_t R_src, int64_t R_tgt, int F, void* z, void* stream);
+
+/* Its gradients: du[src_row_of[t, a], :] = sum over b (ascending) of beta[t, a, b] dz[tgt_row_of[t, b], :] over the paths
+ * (zeros for a source without paths, rows of no pair left as they were); dbeta[t, a, b] = sum over the columns of
+ * dz[tgt_row_of[t, b], :] u[src_row_of[t, a], :], 0 where there is no path. dz [R_tgt,F] and u [R_src,F] of `dtype`, du
+ * [R_src,F] of out_dtype, dbeta [T,k,k] f32. du or dbeta may be NULL: not wanted; u may be NULL without dbeta. */
+pcm_status pcm_mix_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dz, const void* u,
+                             const uint64_t* path_bits, const float* beta, const int32_t* src_row_of,
+                             const int32_t* tgt_row_of, int64_t T, int k, int64_t R_src, int64_t R_tgt, int F,
+                             void* du, float* dbeta, void* stream);
+
+/* The router's gradient: dlogits [T,n] of out_dtype from the gradients of what pcm_route and pcm_build_paths (or
+ * pcm_route_paths) made of the logits: dw [T,k] f32 by topk_w, dbeta [T,k,k] f32 by beta (only the elements of the
+ * paths in path_bits are read), either or both (the others NULL). Logits that were not selected get 0. Computed in
+ * 64 bits from the float32 inputs, rounded to float32, then to out_dtype. */
+pcm_status pcm_route_grad(pcm_dtype out_dtype, const int32_t* topk_ids, const float* topk_w,
+                          const uint64_t* path_bits, const float* dbeta, pcm_beta_mode beta_mode,
+                          const float* dw, int64_t T, int n, int k, void* dlogits, void* stream);
+
+/* A gradient among all of a model's: `count` neighbouring elements of PCM_F32 or PCM_BF16. data need only be aligned
+ * to its elements (a view into a flat buffer); it may be NULL where count is 0. */
+typedef struct pcm_tensor {
+    void* data;
+    int64_t count;      /* at most 2^36 */
+    pcm_dtype dtype;
+} pcm_tensor;
+
+/* The norm over all gradients: norm [1] f32 (device) = sqrt(sum of squares of every element of grads[0, m)), squares and
+ * sums in 64 bits, the norm rounded (over float32's largest: infinite). `grads` is host memory, read before the call returns; m <= 4096.
+ * ws: pcm_workspace_bytes(PCM_OP_GRAD_NORM, m, 0, 0, 1, 1, 0) bytes. */
+pcm_status pcm_grad_norm(const pcm_tensor* grads, int m, float* norm, void* ws, size_t ws_bytes, void* stream);
+
+/* Clipping by a norm on the device (pcm_grad_norm's, or one made of several ranks'): with norm > max_norm, out[i] =
+ * grads[i] * (max_norm / norm), the factor rounded to float32, otherwise out[i] = grads[i]; a norm that is not finite
+ * leaves the values as they are. out: tensors of the same counts, of either type; NULL: in place. Each out[i] is
+ * grads[i] itself or overlaps no other tensor of the call; gradients do not overlap each other. */
+pcm_status pcm_clip_grads(const pcm_tensor* grads, const pcm_tensor* out, int m, const float* norm,
+                          float max_norm, void* stream);
+
+/* Both, with the same results, in one pass of launches less: norm [1] f32 is written. Arguments as above. */
+pcm_status pcm_clip_grad_norm(const pcm_tensor* grads, const pcm_tensor* out, int m, float max_norm,
+                              float* norm, void* ws, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------- tests and measurement
  * A layer never needs these. The *_tuned calls are the calls above with a pcm_tuning that

@@ -16,6 +16,9 @@ from .binding import (BETA_GLOBAL, BETA_PRODUCT, BETA_SRC_COND, PCM_BF16, PCM_BF
                       capture_graph, workspace_bytes)
 from .experts import (pcm_grouped_gemm, pcm_grouped_gemm_dw, pcm_grouped_gemm_dx, pcm_grouped_gemm_fp8,
                       pcm_quant_fp8_rows, pcm_quant_fp8_weights, pcm_swiglu_quant_fp8)
+from .training import (pcm_clip_grad_norm, pcm_clip_grads, pcm_combine_rows, pcm_combine_rows_grad,
+                       pcm_dispatch_rows, pcm_dispatch_rows_grad, pcm_grad_norm, pcm_mix_rows,
+                       pcm_mix_rows_grad, pcm_route_grad, pcm_swiglu, pcm_swiglu_grad)
 
 __all__ = ["BETA_GLOBAL", "BETA_PRODUCT", "BETA_SRC_COND", "PCM_BF16", "PCM_BF16_F16DOWN", "PCM_F32",
            "LayerPlan",
@@ -28,4 +31,7 @@ __all__ = ["BETA_GLOBAL", "BETA_PRODUCT", "BETA_SRC_COND", "PCM_BF16", "PCM_BF16
            "pcm_mask_pack", "pcm_route_paths", "pcm_widen_f16",
            "capture_graph", "workspace_bytes",
            "pcm_grouped_gemm", "pcm_grouped_gemm_dw", "pcm_grouped_gemm_dx", "pcm_grouped_gemm_fp8",
-           "pcm_quant_fp8_rows", "pcm_quant_fp8_weights", "pcm_swiglu_quant_fp8"]
+           "pcm_quant_fp8_rows", "pcm_quant_fp8_weights", "pcm_swiglu_quant_fp8",
+           "pcm_dispatch_rows", "pcm_dispatch_rows_grad", "pcm_combine_rows", "pcm_combine_rows_grad",
+           "pcm_swiglu", "pcm_swiglu_grad", "pcm_mix_rows", "pcm_mix_rows_grad", "pcm_route_grad",
+           "pcm_grad_norm", "pcm_clip_grads", "pcm_clip_grad_norm"]

@@ -22,6 +22,7 @@ PCM_F32, PCM_BF16, PCM_BF16_F16DOWN = 0, 1, 2
 BETA_SRC_COND, BETA_PRODUCT, BETA_GLOBAL = 0, 1, 2
 OP_BUILD_PATHS, OP_EXPAND, OP_PROJECT_COMBINE, OP_DENSE_SWIGLU, OP_ROUTE_SCORED = 0, 1, 2, 3, 4
 OP_LAYER_PER_PATH, OP_ROUTE_LOGITS, OP_ROUTE_PATHS, OP_GROUPED_DX, OP_GROUPED_DW = 5, 6, 7, 8, 9
+OP_GRAD_NORM = 10
 
 EXPORTS = ("pcm_route", "pcm_build_paths", "pcm_expand", "pcm_project_combine",
            "pcm_dense_swiglu", "pcm_workspace_bytes", "pcm_status_string", "pcm_abi_version",
@@ -32,7 +33,10 @@ EXPORTS = ("pcm_route", "pcm_build_paths", "pcm_expand", "pcm_project_combine",
            "pcm_project_workspace_layout", "pcm_project_combine_noalloc", "pcm_mask_pack",
            "pcm_route_paths", "pcm_widen_f16", "pcm_grouped_gemm", "pcm_grouped_gemm_dx",
            "pcm_grouped_gemm_dw", "pcm_quant_fp8_rows", "pcm_swiglu_quant_fp8",
-           "pcm_quant_fp8_weights", "pcm_grouped_gemm_fp8")
+           "pcm_quant_fp8_weights", "pcm_grouped_gemm_fp8", "pcm_dispatch_rows",
+           "pcm_dispatch_rows_grad", "pcm_combine_rows", "pcm_combine_rows_grad", "pcm_swiglu",
+           "pcm_swiglu_grad", "pcm_mix_rows", "pcm_mix_rows_grad", "pcm_route_grad", "pcm_grad_norm",
+           "pcm_clip_grads", "pcm_clip_grad_norm")
 
 
 class PcmTuning(ctypes.Structure):
@@ -126,6 +130,18 @@ def lib(path: str = _LIB_PATH) -> ctypes.CDLL:
     L.pcm_swiglu_quant_fp8.argtypes = [I, P, P, I64, I, P, P, P]
     L.pcm_quant_fp8_weights.argtypes = [I, P, I, I, I, P, P, P, P, P]
     L.pcm_grouped_gemm_fp8.argtypes = [I, P, P, P, P, P, P, I64, I64, I, I, I, P, P]
+    L.pcm_dispatch_rows.argtypes = [I, I, P, P, P, P, I64, I, I64, I, I, P, P]
+    L.pcm_dispatch_rows_grad.argtypes = [I, I, P, P, P, P, P, I64, I, I64, I, I, P, P, P]
+    L.pcm_combine_rows.argtypes = [I, I, P, P, P, P, I64, I, I64, I, I, P, I, P]
+    L.pcm_combine_rows_grad.argtypes = L.pcm_dispatch_rows_grad.argtypes
+    L.pcm_swiglu.argtypes = [I, I, P, P, I64, I, P, P]
+    L.pcm_swiglu_grad.argtypes = [I, I, P, P, P, I64, I, P, P]
+    L.pcm_mix_rows.argtypes = [I, I, P, P, P, P, P, I64, I, I64, I64, I, P, P]
+    L.pcm_mix_rows_grad.argtypes = [I, I, P, P, P, P, P, P, I64, I, I64, I64, I, P, P, P]
+    L.pcm_route_grad.argtypes = [I, P, P, P, P, I, P, I64, I, I, P, P]
+    L.pcm_grad_norm.argtypes = [P, I, P, P, SZ, P]
+    L.pcm_clip_grads.argtypes = [P, P, I, P, ctypes.c_float, P]
+    L.pcm_clip_grad_norm.argtypes = [P, P, I, ctypes.c_float, P, P, SZ, P]
     TP = ctypes.POINTER(PcmTuning)
     for name in ("pcm_expand", "pcm_project_combine", "pcm_dense_swiglu", "pcm_expand_scored",
                  "pcm_project_combine_scored"):
@@ -144,7 +160,10 @@ def lib(path: str = _LIB_PATH) -> ctypes.CDLL:
                  "pcm_project_workspace_layout", "pcm_project_combine_noalloc", "pcm_mask_pack",
                  "pcm_route_paths", "pcm_widen_f16", "pcm_grouped_gemm", "pcm_grouped_gemm_dx",
                  "pcm_grouped_gemm_dw", "pcm_quant_fp8_rows", "pcm_swiglu_quant_fp8",
-                 "pcm_quant_fp8_weights", "pcm_grouped_gemm_fp8"):
+                 "pcm_quant_fp8_weights", "pcm_grouped_gemm_fp8", "pcm_dispatch_rows",
+                 "pcm_dispatch_rows_grad", "pcm_combine_rows", "pcm_combine_rows_grad", "pcm_swiglu",
+                 "pcm_swiglu_grad", "pcm_mix_rows", "pcm_mix_rows_grad", "pcm_route_grad",
+                 "pcm_grad_norm", "pcm_clip_grads", "pcm_clip_grad_norm"):
         getattr(L, name).restype = I
     _lib = L
     return L

@@ -6,6 +6,7 @@
 // 2 x 1408 41 us (5.7), 64 weights of 2048 x 1024 with their transposes 104 us (5.1 of the 5.1 TB/s that a
 // copy has). The product: 8192^3 2060 TF into bf16; 8 experts of 14336 x 4096 with 8192 rows 560-580 us; 256
 // of 2048 x 7168 with one row each 345-360 us (weights at 6.7-7 TB/s).
+#include "eight.h"
 #include "grouped.h"
 
 namespace pcm {
@@ -15,30 +16,11 @@ constexpr float kE4m3Max = 448.0f;
 constexpr float kFloor = 0x1p-100f;
 
 typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
-typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 
 // magnitude bits of v, 0 for infinities and NaN
 __device__ __forceinline__ uint32_t finite_bits(float v) {
     const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
     return b < 0x7F800000u ? b : 0u;
-}
-
-struct Eight {
-    float v[8];
-};
-__device__ __forceinline__ Eight load8(const uint16_t* p) {
-    const uintx4 w = *(const uintx4*)p;
-    Eight r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r.v[2 * i] = __uint_as_float(w[i] << 16);
-        r.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-    return r;
-}
-__device__ __forceinline__ Eight load8(const float* p) {
-    const floatx4 a = *(const floatx4*)p, b = *(const floatx4*)(p + 4);
-    return Eight{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
 
 template <bool FINITE>
@@ -69,29 +51,6 @@ __device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d
 __device__ __forceinline__ uintx2 eight_e4m3(const Eight& x, float inv) {
     return uintx2{four_e4m3(x.v[0] * inv, x.v[1] * inv, x.v[2] * inv, x.v[3] * inv),
                   four_e4m3(x.v[4] * inv, x.v[5] * inv, x.v[6] * inv, x.v[7] * inv)};
-}
-
-// SiLU(g) u in float32, near to correctly rounded: an error of some units in the last place would move as many
-// more codes across a border between two. g / (1 + e^-g) alone would lose the gates from -88.8 down, whose
-// exponential is infinite, and with the reciprocal instruction, whose results are never below the normal range, those
-// from -87.4; SiLU(g) u is a plain number there where u is large.
-// bf16 inputs (this is what the kernel has time for next to its memory traffic): e^-g = 2^i 2^f with i whole and f
-// from fused multiply-adds (2^(-g log2 e) at once is off by |g| units), the hardware reciprocal (about 1 ulp), and
-// both terms of the sum smaller by 2^60. i - 60 comes in the low bits of a sum with 1.5 2^23 and is added to the
-// exponent; the bounds keep that exponent in range and do not change the result (e^-40 is nothing beside 1, and
-// from g = -120 down the result is 0). 32768 x 2 x 1408: 40 us, as with neither; a choice between two forms 42.7.
-// float32 inputs: the library exponential and an IEEE division; below -80 1 + e^g is 1 and SiLU(g) = g e^g.
-__device__ __forceinline__ float gated(uint16_t, float g, float u) {
-    constexpr float kLog2e = 1.44269504088896340736f, kWhole = 0x1.8p23f - 60.0f, kDown = 0x1p-60f;
-    const float c = __builtin_amdgcn_fmed3f(-g, -40.0f, 120.0f);
-    const float n = fmaf(c, kLog2e, kWhole), f = fmaf(c, kLog2e, kWhole - n);
-    const float e = __uint_as_float(__float_as_uint(__builtin_amdgcn_exp2f(f)) + (__float_as_uint(n) << 23));
-    return g * (__builtin_amdgcn_rcpf(kDown + e) * kDown) * u;
-}
-__device__ __forceinline__ float gated(float, float g, float u) {
-    const bool far = g < -80.0f;
-    const float e = expf(far ? g : -g);
-    return (far ? g * e : g / (1.0f + e)) * u;
 }
 
 // Rows in blocks of 128 columns: 16 lanes take a block, 8 values each; the maximum stays in registers.

@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+struct pcm_tensor;
+
 namespace pcm {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -287,5 +289,64 @@ hipError_t launch_quant_rows(bool bf16, bool swiglu, const void* x, const int32_
                              float* scale, hipStream_t s);
 hipError_t launch_quant_weights(bool bf16, const void* w, int n, int N, int K, uint8_t* q, float* scale, uint8_t* q_t,
                                 float* scale_t, hipStream_t s);
+
+// Tokens to rows and back (rows.hip): rows r = row_of[t * k + a] of the groups, others have no part.
+struct RowsArgs {
+    const void* tokens;       // [T, H] (dispatch: x, its gradient: x or NULL, combine's gradient: dy)
+    const void* rows;         // [R, H] (dispatch's gradient: dy, combine: o, its gradient: o or NULL)
+    void* out;                // rows or tokens (NULL: only dweights)
+    const int32_t* row_of;
+    const float* weights;     // [T, k] (NULL: 1)
+    float* dweights;          // [T, k] (NULL: not wanted)
+    const int32_t* offsets;   // [n + 1] (NULL: all R rows)
+    int64_t T, R;
+    int k, H, n;
+    int accumulate;           // combine: add into out
+};
+hipError_t launch_rows(bool to_rows, bool bf16, bool out_bf16, const RowsArgs& g, hipStream_t s);
+// The mix along a token's paths and its gradient.
+struct MixRowsArgs {
+    const void* u;            // [R_src, F] (gradient: NULL where dbeta is not wanted)
+    const void* dz;           // gradient: [R_tgt, F]
+    void* out;                // z [R_tgt, F], or du [R_src, F] (NULL: not wanted)
+    float* dbeta;             // gradient: [T, k, k] (NULL: not wanted)
+    const uint64_t* bits;
+    const float* beta;
+    const int32_t* src_row_of;
+    const int32_t* tgt_row_of;
+    int64_t T, R_src, R_tgt;
+    int k, F;
+};
+hipError_t launch_mix_rows(bool grad, bool bf16, bool out_bf16, const MixRowsArgs& g, hipStream_t s);
+// u = SiLU(gate) * up, or, with du, the gradient by gate_up (swiglu.hip).
+hipError_t launch_swiglu(bool bf16, bool out_bf16, const void* gate_up, const void* du, const int32_t* count, int64_t R, int F,
+                         void* out, hipStream_t s);
+// The gradient by the logits (grads.hip).
+struct RouteGradArgs {
+    const int32_t* ids;       // [T, k]
+    const float* w;           // [T, k]
+    const uint64_t* bits;     // [T] and dbeta [T, k, k], or both NULL
+    const float* dbeta;
+    const float* dw;          // [T, k] or NULL
+    void* dlogits;            // [T, n]
+    int64_t T;
+    int n, k, beta_mode;
+};
+hipError_t launch_route_grad(bool out_bf16, const RouteGradArgs& g, hipStream_t s);
+// The norm over tensors and clipping. A table of them is passed by value, up to kMost a launch.
+struct GradTable {
+    static constexpr int kMost = 96;
+    const void* src[kMost];
+    void* dst[kMost];
+    int64_t count[kMost];
+    uint32_t start[kMost + 1];   // first chunk of each
+    uint8_t type[kMost];         // bit 0: src is bf16, bit 1: dst is
+    int m;
+};
+constexpr int kGradBlocks = 2048;   // workgroups of a launch
+size_t grad_norm_ws_bytes(int64_t m);
+// parts: the norm is formed (in grad_norm_ws_bytes(m)) and written, otherwise read; clip: out (NULL: in) = in * factor.
+hipError_t launch_grad_norm(const pcm_tensor* in, const pcm_tensor* out, int m, bool clip, float max_norm, float* norm, double* parts,
+                            hipStream_t s);
 
 }  // namespace pcm

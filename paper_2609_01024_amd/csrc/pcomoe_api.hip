@@ -3,6 +3,7 @@
 // synchronises.
 #include "pcomoe.h"
 
+#include <algorithm>
 #include <mutex>
 
 #include "internal.h"
@@ -77,6 +78,56 @@ bool grouped_rows(const int32_t* offsets, const int32_t* row_token, int64_t T, i
     if (!offsets && (n != 1 || row_token)) return false;
     if (!row_token && T != R) return false;
     return !(row_token && T == 0 && R > 0) && aligned16(offsets) && aligned16(row_token);
+}
+
+// Training around the products: sizes, then what the calls on rows share.
+pcm_status check_rows(int64_t T, int64_t R, int k, int H, int n) {
+    const pcm_status st = check_grouped(T, R, H, 16, n);
+    if (st != PCM_OK) return st;
+    if (k < 1) return PCM_ERR_ARG;
+    return k > kMaxK ? PCM_ERR_UNSUPPORTED : PCM_OK;
+}
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }   // any element of an array of 32-bit numbers
+
+constexpr int kMaxTensors = 4096;
+constexpr int64_t kMaxTensor = (int64_t)1 << 36;
+pcm_status check_tensors(const pcm_tensor* t, int m) {
+    for (int i = 0; i < m; ++i) {
+        if (!plain_dtype(t[i].dtype) || t[i].count < 0) return PCM_ERR_ARG;
+        if (t[i].count > kMaxTensor) return PCM_ERR_UNSUPPORTED;
+        const uintptr_t size = t[i].dtype == PCM_BF16 ? 2 : 4;
+        if (t[i].count && (!t[i].data || (uintptr_t)t[i].data % size)) return PCM_ERR_ARG;
+    }
+    return PCM_OK;
+}
+// Whether two tensors of a call share memory, an output with its own gradient aside (then of the same type).
+bool overlapping(const pcm_tensor* in, const pcm_tensor* out, int m) {
+    struct Range {
+        uintptr_t from, to;
+    } r[2 * kMaxTensors];
+    int count = 0;
+    for (const pcm_tensor* t : {in, out})
+        for (int i = 0; t && i < m; ++i) {
+            if (!t[i].count || (t == out && t[i].data == in[i].data && t[i].dtype == in[i].dtype)) continue;
+            const uintptr_t from = (uintptr_t)t[i].data;
+            r[count++] = Range{from, from + (uintptr_t)t[i].count * (t[i].dtype == PCM_BF16 ? 2 : 4)};
+        }
+    std::sort(r, r + count, [](const Range& a, const Range& b) { return a.from < b.from; });
+    for (int i = 1; i < count; ++i)
+        if (r[i].from < r[i - 1].to) return true;
+    return false;
+}
+pcm_status check_clip(const pcm_tensor* grads, const pcm_tensor* out, int m, float max_norm) {
+    if (m < 0 || !(max_norm >= 0.0f)) return PCM_ERR_ARG;
+    if (m > kMaxTensors) return PCM_ERR_UNSUPPORTED;
+    if (m == 0) return PCM_OK;
+    if (!grads) return PCM_ERR_ARG;
+    pcm_status st = check_tensors(grads, m);
+    if (st == PCM_OK && out) st = check_tensors(out, m);
+    if (st != PCM_OK) return st;
+    for (int i = 0; out && i < m; ++i)
+        if (out[i].count != grads[i].count) return PCM_ERR_ARG;
+    return overlapping(grads, out == grads ? nullptr : out, m) ? PCM_ERR_ARG : PCM_OK;
 }
 
 pcm_status from_hip(hipError_t e) { return e == hipSuccess ? PCM_OK : PCM_ERR_HIP; }
@@ -210,6 +261,7 @@ size_t pcm_workspace_bytes(pcm_op op, int64_t T, int H, int F, int n, int k, pcm
             const int parts = dw_parts(T * k, F, H, n);
             return parts > 1 ? (size_t)parts * n * H * F * sizeof(float) : 0;
         }
+        case PCM_OP_GRAD_NORM: return grad_norm_ws_bytes(T);  // T tensors: the workgroups' sums
         case PCM_OP_ROUTE_SCORED:  // block counts of the source and the target dispatch
             return 2 * build_paths_ws_bytes(T, n);
         case PCM_OP_DENSE_SWIGLU:  // the SwiGLU output u [T,F] f32, then a projection input
@@ -902,6 +954,191 @@ pcm_status pcm_grouped_gemm_fp8(pcm_dtype out_dtype, const uint8_t* x, const flo
     g.len = K;
     g.cols = N;
     return from_hip(launch_grouped_fp8(out_dtype == PCM_BF16, g, (hipStream_t)stream));
+}
+
+static pcm_status rows_call(bool to_rows, pcm_dtype dtype, pcm_dtype out_dtype, const void* tokens, const void* rows,
+                            const int32_t* row_of, const float* weights, const int32_t* offsets, int64_t T, int k,
+                            int64_t R, int H, int n, void* out, float* dweights, bool dot, int accumulate, void* stream) {
+    const pcm_status st = check_rows(T, R, k, H, n);
+    if (st != PCM_OK) return st;
+    if (!plain_dtype(dtype) || !plain_dtype(out_dtype) || (!offsets && n != 1)) return PCM_ERR_ARG;
+    if (accumulate && out_dtype != PCM_F32) return PCM_ERR_ARG;
+    if (!aligned16(tokens) || !aligned16(rows) || !aligned16(row_of) || !aligned16(weights) || !aligned4(offsets) ||
+        !aligned16(out) || !aligned16(dweights))
+        return PCM_ERR_ARG;
+    // (row buffers without rows may be NULL)
+    if (T == 0 || (to_rows && R == 0 && !dweights)) return PCM_OK;
+    if (!row_of || (!out && !dweights) || (!dot && !out)) return PCM_ERR_ARG;
+    if (!tokens && ((to_rows && R > 0) || dweights)) return PCM_ERR_ARG;
+    if (!rows && R > 0 && (!to_rows || dweights)) return PCM_ERR_ARG;
+    RowsArgs g{};
+    g.tokens = tokens;
+    g.rows = rows;
+    g.out = out;
+    g.row_of = row_of;
+    g.weights = weights;
+    g.dweights = dweights;
+    g.offsets = offsets;
+    g.T = T;
+    g.R = R;
+    g.k = k;
+    g.H = H;
+    g.n = n;
+    g.accumulate = accumulate != 0;
+    return from_hip(launch_rows(to_rows, dtype == PCM_BF16, out_dtype == PCM_BF16, g, (hipStream_t)stream));
+}
+
+pcm_status pcm_dispatch_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const int32_t* row_of,
+                             const float* weights, const int32_t* offsets, int64_t T, int k, int64_t R,
+                             int H, int n, void* y, void* stream) {
+    return rows_call(true, dtype, out_dtype, x, nullptr, row_of, weights, offsets, T, k, R, H, n, y, nullptr, false, 0, stream);
+}
+
+pcm_status pcm_dispatch_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* x,
+                                  const int32_t* row_of, const float* weights, const int32_t* offsets,
+                                  int64_t T, int k, int64_t R, int H, int n, void* dx, float* dweights,
+                                  void* stream) {
+    return rows_call(false, dtype, out_dtype, x, dy, row_of, weights, offsets, T, k, R, H, n, dx, dweights, true, 0, stream);
+}
+
+pcm_status pcm_combine_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* o, const int32_t* row_of,
+                            const float* weights, const int32_t* offsets, int64_t T, int k, int64_t R,
+                            int H, int n, void* y, int accumulate, void* stream) {
+    return rows_call(false, dtype, out_dtype, nullptr, o, row_of, weights, offsets, T, k, R, H, n, y, nullptr, false, accumulate,
+                     stream);
+}
+
+pcm_status pcm_combine_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* o,
+                                 const int32_t* row_of, const float* weights, const int32_t* offsets,
+                                 int64_t T, int k, int64_t R, int H, int n, void* d_o, float* dweights,
+                                 void* stream) {
+    return rows_call(true, dtype, out_dtype, dy, o, row_of, weights, offsets, T, k, R, H, n, d_o, dweights, true, 0, stream);
+}
+
+static pcm_status swiglu_call(pcm_dtype dtype, pcm_dtype out_dtype, const void* gate_up, const void* du, bool grad,
+                              const int32_t* count, int64_t R, int F, void* out, void* stream) {
+    const pcm_status st = check_rows(0, R, 1, F, 1);
+    if (st != PCM_OK) return st;
+    if (!plain_dtype(dtype) || !plain_dtype(out_dtype)) return PCM_ERR_ARG;
+    if (R == 0) return PCM_OK;
+    if (!gate_up || !out || (grad && !du) || !aligned16(gate_up) || !aligned16(du) || !aligned16(out) || !aligned4(count))
+        return PCM_ERR_ARG;
+    return from_hip(launch_swiglu(dtype == PCM_BF16, out_dtype == PCM_BF16, gate_up, du, count, R, F, out, (hipStream_t)stream));
+}
+
+pcm_status pcm_swiglu(pcm_dtype dtype, pcm_dtype out_dtype, const void* gate_up, const int32_t* count,
+                      int64_t R, int F, void* u, void* stream) {
+    return swiglu_call(dtype, out_dtype, gate_up, nullptr, false, count, R, F, u, stream);
+}
+
+pcm_status pcm_swiglu_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* gate_up, const void* du,
+                           const int32_t* count, int64_t R, int F, void* dgate_up, void* stream) {
+    return swiglu_call(dtype, out_dtype, gate_up, du, true, count, R, F, dgate_up, stream);
+}
+
+static pcm_status mix_call(bool grad, pcm_dtype dtype, pcm_dtype out_dtype, const void* u, const void* dz,
+                           const uint64_t* path_bits, const float* beta, const int32_t* src_row_of,
+                           const int32_t* tgt_row_of, int64_t T, int k, int64_t R_src, int64_t R_tgt, int F, void* out,
+                           float* dbeta, void* stream) {
+    pcm_status st = check_rows(T, R_src, k, F, 1);
+    if (st == PCM_OK) st = check_rows(T, R_tgt, k, F, 1);
+    if (st != PCM_OK) return st;
+    if (!plain_dtype(dtype) || !plain_dtype(out_dtype)) return PCM_ERR_ARG;
+    if (!aligned16(u) || !aligned16(dz) || !aligned16(path_bits) || !aligned16(beta) || !aligned16(src_row_of) ||
+        !aligned16(tgt_row_of) || !aligned16(out) || !aligned16(dbeta))
+        return PCM_ERR_ARG;
+    if (T == 0 || ((grad ? R_src : R_tgt) == 0 && !dbeta)) return PCM_OK;   // (buffers without rows may be NULL)
+    if (!path_bits || !beta || !src_row_of || !tgt_row_of || (!out && !dbeta)) return PCM_ERR_ARG;
+    if (!u && R_src > 0 && (!grad || dbeta)) return PCM_ERR_ARG;
+    if (!dz && grad && R_tgt > 0) return PCM_ERR_ARG;
+    MixRowsArgs g{};
+    g.u = u;
+    g.dz = dz;
+    g.out = out;
+    g.dbeta = dbeta;
+    g.bits = path_bits;
+    g.beta = beta;
+    g.src_row_of = src_row_of;
+    g.tgt_row_of = tgt_row_of;
+    g.T = T;
+    g.R_src = R_src;
+    g.R_tgt = R_tgt;
+    g.k = k;
+    g.F = F;
+    return from_hip(launch_mix_rows(grad, dtype == PCM_BF16, out_dtype == PCM_BF16, g, (hipStream_t)stream));
+}
+
+pcm_status pcm_mix_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* u, const uint64_t* path_bits,
+                        const float* beta, const int32_t* src_row_of, const int32_t* tgt_row_of, int64_t T,
+                        int k, int64_t R_src, int64_t R_tgt, int F, void* z, void* stream) {
+    return mix_call(false, dtype, out_dtype, u, nullptr, path_bits, beta, src_row_of, tgt_row_of, T, k, R_src, R_tgt, F, z,
+                    nullptr, stream);
+}
+
+pcm_status pcm_mix_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dz, const void* u,
+                             const uint64_t* path_bits, const float* beta, const int32_t* src_row_of,
+                             const int32_t* tgt_row_of, int64_t T, int k, int64_t R_src, int64_t R_tgt, int F,
+                             void* du, float* dbeta, void* stream) {
+    return mix_call(true, dtype, out_dtype, u, dz, path_bits, beta, src_row_of, tgt_row_of, T, k, R_src, R_tgt, F, du, dbeta,
+                    stream);
+}
+
+pcm_status pcm_route_grad(pcm_dtype out_dtype, const int32_t* topk_ids, const float* topk_w,
+                          const uint64_t* path_bits, const float* dbeta, pcm_beta_mode beta_mode,
+                          const float* dw, int64_t T, int n, int k, void* dlogits, void* stream) {
+    const pcm_status st = check_shape(T, n, k);
+    if (st != PCM_OK) return st;
+    if (!plain_dtype(out_dtype) || beta_mode < PCM_BETA_SRC_COND || beta_mode > PCM_BETA_GLOBAL) return PCM_ERR_ARG;
+    if (T >= kMaxGroupedRows) return PCM_ERR_UNSUPPORTED;
+    if (!aligned16(topk_ids) || !aligned16(topk_w) || !aligned16(path_bits) || !aligned16(dbeta) || !aligned16(dw) ||
+        !aligned16(dlogits) || !path_bits != !dbeta)
+        return PCM_ERR_ARG;
+    if (T == 0) return PCM_OK;
+    if (!topk_ids || !topk_w || !dlogits || (!dbeta && !dw)) return PCM_ERR_ARG;
+    RouteGradArgs g{};
+    g.ids = topk_ids;
+    g.w = topk_w;
+    g.bits = path_bits;
+    g.dbeta = dbeta;
+    g.dw = dw;
+    g.dlogits = dlogits;
+    g.T = T;
+    g.n = n;
+    g.k = k;
+    g.beta_mode = (int)beta_mode;
+    return from_hip(launch_route_grad(out_dtype == PCM_BF16, g, (hipStream_t)stream));
+}
+
+static pcm_status check_norm(int m, const float* norm, const void* ws, size_t ws_bytes) {
+    if (!norm || !aligned4(norm)) return PCM_ERR_ARG;
+    if (ws_bytes < pcm_workspace_bytes(PCM_OP_GRAD_NORM, m, 0, 0, 1, 1, PCM_F32) || !ws) return PCM_ERR_WORKSPACE;
+    return aligned16(ws) ? PCM_OK : PCM_ERR_ARG;
+}
+
+pcm_status pcm_grad_norm(const pcm_tensor* grads, int m, float* norm, void* ws, size_t ws_bytes, void* stream) {
+    if (m < 0 || (m && !grads)) return PCM_ERR_ARG;
+    if (m > kMaxTensors) return PCM_ERR_UNSUPPORTED;
+    pcm_status st = check_tensors(grads, m);
+    if (st == PCM_OK) st = check_norm(m, norm, ws, ws_bytes);
+    if (st != PCM_OK) return st;
+    return from_hip(launch_grad_norm(grads, nullptr, m, false, 0.0f, norm, (double*)ws, (hipStream_t)stream));
+}
+
+pcm_status pcm_clip_grads(const pcm_tensor* grads, const pcm_tensor* out, int m, const float* norm,
+                          float max_norm, void* stream) {
+    const pcm_status st = check_clip(grads, out, m, max_norm);
+    if (st != PCM_OK) return st;
+    if (m == 0) return PCM_OK;
+    if (!norm || !aligned4(norm)) return PCM_ERR_ARG;
+    return from_hip(launch_grad_norm(grads, out, m, true, max_norm, (float*)norm, nullptr, (hipStream_t)stream));
+}
+
+pcm_status pcm_clip_grad_norm(const pcm_tensor* grads, const pcm_tensor* out, int m, float max_norm,
+                              float* norm, void* ws, size_t ws_bytes, void* stream) {
+    pcm_status st = check_clip(grads, out, m, max_norm);
+    if (st == PCM_OK) st = check_norm(m, norm, ws, ws_bytes);
+    if (st != PCM_OK) return st;
+    return from_hip(launch_grad_norm(grads, out, m, true, max_norm, norm, (double*)ws, (hipStream_t)stream));
 }
 
 }  // extern "C"
