@@ -88,9 +88,11 @@ __global__ __launch_bounds__(kTokens * kMaxK) void route_grad_kernel(RouteGradAr
 }
 
 // ---------------------------------------------------------------- all gradients
-// A launch takes up to GradTable::kMost tensors, cut into chunks of kChunk elements; a workgroup takes a run of
-// neighbouring chunks. Squares and their sums are 64 bits: no gradient that float32 holds overflows or vanishes in them.
-constexpr int kChunk = 4096, kNormThreads = 256;
+// A launch takes up to GradTable::kMost tensors, cut into chunks of 16 KB (of what is read) that begin at multiples of 16
+// bytes, wherever the tensor does: four 16-byte vectors a thread. The vectors at a tensor's ends that hold other bytes
+// too go by elements. Squares and their sums are 64 bits: no gradient that float32 holds overflows or vanishes in them.
+constexpr int kChunk = 16384, kNormThreads = 256, kVectors = kChunk / 16 / kNormThreads;
+constexpr int kFewParts = 256;   // sums that every workgroup of the clipping adds itself, instead of a launch that does
 
 __device__ __forceinline__ double block_sum(double v, double* part) {
 #pragma unroll
@@ -115,31 +117,83 @@ __device__ __forceinline__ int tensor_of(const GradTable& g, uint32_t c) {
     return lo;
 }
 
+template <class T>
+struct Vec;   // the elements of 16 bytes
+template <>
+struct Vec<uint16_t> {
+    static constexpr int N = 8;
+    float v[8];
+};
+template <>
+struct Vec<float> {
+    static constexpr int N = 4;
+    float v[4];
+};
+__device__ __forceinline__ Vec<uint16_t> unpacked(const uint16_t*, uintx4 w) {
+    Vec<uint16_t> r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r.v[2 * i] = __uint_as_float(w[i] << 16);
+        r.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+    return r;
+}
+__device__ __forceinline__ Vec<float> unpacked(const float*, uintx4 w) {
+    return Vec<float>{{__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3])}};
+}
 __device__ __forceinline__ float element(const uint16_t* p, int64_t i) { return bf16_bits_to_f32(p[i]); }
 __device__ __forceinline__ float element(const float* p, int64_t i) { return p[i]; }
 __device__ __forceinline__ void put(uint16_t* p, int64_t i, float v) { p[i] = __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ void put(float* p, int64_t i, float v) { p[i] = v; }
 
-template <class IN>
-__device__ __forceinline__ double chunk_squares(const IN* p, int64_t lo, int64_t hi) {
-    double s = 0.0;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += kNormThreads) {
-        const double v = (double)element(p, i);
-        s = fma(v, v, s);
+// Chunk j of a tensor of `count` elements at p: whole(first element, vector) for each vector inside, part(element) for
+// each element of the others. All vectors are loaded first.
+template <class T, class WHOLE, class PART>
+__device__ __forceinline__ void each_vector(const T* p, int64_t count, int64_t j, WHOLE whole, PART part) {
+    constexpr int N = Vec<T>::N;
+    const int64_t before = ((uintptr_t)p & 15) / sizeof(T);     // elements of the first vector that lie before p
+    const int64_t e0 = j * (kChunk / (int64_t)sizeof(T)) - before + threadIdx.x * N;
+    uintx4 w[kVectors];
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+        const int64_t e = e0 + i * (kNormThreads * N);
+        if (e >= 0 && e + N <= count) w[i] = __builtin_nontemporal_load((const uintx4*)(p + e));
     }
-    return s;
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+        const int64_t e = e0 + i * (kNormThreads * N);
+        if (e >= 0 && e + N <= count) whole(e, unpacked(p, w[i]));
+        else
+            for (int q = 0; q < N; ++q)
+                if (e + q >= 0 && e + q < count) part(e + q);
+    }
 }
 
-__global__ __launch_bounds__(kNormThreads) void norm_kernel(GradTable g, uint32_t per, double* __restrict__ parts) {
+template <class T>
+__device__ __forceinline__ double chunk_squares(const T* p, int64_t count, int64_t j) {
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    each_vector(
+        p, count, j,
+        [&](int64_t, const Vec<T>& x) {
+#pragma unroll
+            for (int i = 0; i < Vec<T>::N; ++i) s[i % 4] = fma((double)x.v[i], (double)x.v[i], s[i % 4]);
+        },
+        [&](int64_t e) {
+            const double v = (double)element(p, e);
+            s[0] = fma(v, v, s[0]);
+        });
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+__global__ __launch_bounds__(kNormThreads) void norm_kernel(GradTable g, double* __restrict__ parts) {
     __shared__ double red[kNormThreads / 64];
     const uint32_t chunks = g.start[g.m];
-    const uint32_t from = blockIdx.x * per, to = min(chunks, from + per);
     double sum = 0.0;
-    int i = from < to ? tensor_of(g, from) : 0;
-    for (uint32_t c = from; c < to; ++c) {
+    int i = tensor_of(g, blockIdx.x);
+    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
         while (c >= g.start[i + 1]) ++i;
-        const int64_t lo = (int64_t)(c - g.start[i]) * kChunk, hi = min(g.count[i], lo + kChunk);
-        sum += g.type[i] & 1 ? chunk_squares((const uint16_t*)g.src[i], lo, hi) : chunk_squares((const float*)g.src[i], lo, hi);
+        const int64_t j = c - g.start[i];
+        sum += g.type[i] & 1 ? chunk_squares((const uint16_t*)g.src[i], g.count[i], j) : chunk_squares((const float*)g.src[i], g.count[i], j);
     }
     sum = block_sum(sum, red);
     if (threadIdx.x == 0) parts[blockIdx.x] = sum;
@@ -159,13 +213,37 @@ __global__ __launch_bounds__(kNormThreads) void norm_join_kernel(const double* _
 }
 
 template <class IN, class OUT>
-__device__ __forceinline__ void chunk_scaled(const IN* p, OUT* q, int64_t lo, int64_t hi, float f) {
-    for (int64_t i = lo + threadIdx.x; i < hi; i += kNormThreads) put(q, i, element(p, i) * f);
+__device__ __forceinline__ void chunk_scaled(const IN* p, OUT* q, int64_t count, int64_t j, float f) {
+    constexpr int N = Vec<IN>::N, kBytes = N * (int)sizeof(OUT) < 16 ? N * (int)sizeof(OUT) : 16;
+    // (an output whose elements lie otherwise than the input's to multiples of a vector)
+    const bool aligned = (((uintptr_t)q - ((uintptr_t)p & 15) / sizeof(IN) * sizeof(OUT)) & (kBytes - 1)) == 0;
+    each_vector(
+        p, count, j,
+        [&](int64_t e, const Vec<IN>& x) {
+            if (!aligned) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) put(q, e + i, x.v[i] * f);
+                return;
+            }
+            if constexpr (sizeof(OUT) == 4) {
+#pragma unroll
+                for (int i = 0; i < N; i += 4)
+                    *(floatx4*)(q + e + i) = floatx4{x.v[i] * f, x.v[i + 1] * f, x.v[i + 2] * f, x.v[i + 3] * f};
+            } else {
+                typedef __bf16 out_t __attribute__((ext_vector_type(N)));
+                out_t y;
+#pragma unroll
+                for (int i = 0; i < N; ++i) y[i] = (__bf16)(x.v[i] * f);
+                *(out_t*)(q + e) = y;
+            }
+        },
+        [&](int64_t e) { put(q, e, element(p, e) * f); });
 }
 
-// parts: the norm is formed from them here (and written by the first workgroup); otherwise it is read.
-__global__ __launch_bounds__(kNormThreads) void clip_kernel(GradTable g, uint32_t per, const double* parts, int count, float* norm,
-                                                            int write_norm, float max_norm) {
+// parts: the norm is formed from them here (and written by the first workgroup); otherwise it is read. A chunk a
+// workgroup: writing goes at 6.5 TB/s read and written that way, at 5 with workgroups that loop.
+__global__ __launch_bounds__(kNormThreads) void clip_kernel(GradTable g, const double* parts, int count, float* norm, int write_norm,
+                                                            float max_norm) {
     __shared__ double red[kNormThreads / 64];
     const float v = parts ? norm_of(parts, count, red) : *norm;
     if (parts && write_norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = v;
@@ -173,41 +251,34 @@ __global__ __launch_bounds__(kNormThreads) void clip_kernel(GradTable g, uint32_
     const bool clip = v > max_norm && v < __builtin_inff();
     const float f = clip ? (float)((double)max_norm / (double)v) : 1.0f;
     const uint32_t chunks = g.start[g.m];
-    const uint32_t from = blockIdx.x * per, to = min(chunks, from + per);
-    int i = from < to ? tensor_of(g, from) : 0;
-    for (uint32_t c = from; c < to; ++c) {
-        while (c >= g.start[i + 1]) ++i;
+    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const int i = tensor_of(g, c);
         if (!clip && g.dst[i] == g.src[i]) continue;
-        const int64_t lo = (int64_t)(c - g.start[i]) * kChunk, hi = min(g.count[i], lo + kChunk);
+        const int64_t j = c - g.start[i], n = g.count[i];
         switch (g.type[i]) {
-            case 0: chunk_scaled((const float*)g.src[i], (float*)g.dst[i], lo, hi, f); break;
-            case 1: chunk_scaled((const uint16_t*)g.src[i], (float*)g.dst[i], lo, hi, f); break;
-            case 2: chunk_scaled((const float*)g.src[i], (uint16_t*)g.dst[i], lo, hi, f); break;
-            default: chunk_scaled((const uint16_t*)g.src[i], (uint16_t*)g.dst[i], lo, hi, f); break;
+            case 0: chunk_scaled((const float*)g.src[i], (float*)g.dst[i], n, j, f); break;
+            case 1: chunk_scaled((const uint16_t*)g.src[i], (float*)g.dst[i], n, j, f); break;
+            case 2: chunk_scaled((const float*)g.src[i], (uint16_t*)g.dst[i], n, j, f); break;
+            default: chunk_scaled((const uint16_t*)g.src[i], (uint16_t*)g.dst[i], n, j, f); break;
         }
     }
 }
 
-// The table of grads[0, m), and the workgroups that share its chunks.
-struct Launch {
-    GradTable table;
-    uint32_t per, blocks;
-};
-bool launch_of(const pcm_tensor* in, const pcm_tensor* out, int m, Launch* l) {
+// The table of grads[0, m); false where its chunks are too many to count.
+bool table_of(const pcm_tensor* in, const pcm_tensor* out, int m, GradTable* g) {
     uint64_t chunks = 0;
-    l->table.m = m;
+    g->m = m;
     for (int i = 0; i < m; ++i) {
-        l->table.src[i] = in[i].data;
-        l->table.dst[i] = out ? out[i].data : in[i].data;
-        l->table.count[i] = in[i].count;
-        l->table.type[i] = (uint8_t)((in[i].dtype == PCM_BF16 ? 1 : 0) | ((out ? out[i] : in[i]).dtype == PCM_BF16 ? 2 : 0));
-        l->table.start[i] = (uint32_t)chunks;
-        chunks += (uint64_t)ceil_div(in[i].count, kChunk);
+        const int64_t size = in[i].dtype == PCM_BF16 ? 2 : 4;
+        g->src[i] = in[i].data;
+        g->dst[i] = out ? out[i].data : in[i].data;
+        g->count[i] = in[i].count;
+        g->type[i] = (uint8_t)((in[i].dtype == PCM_BF16 ? 1 : 0) | ((out ? out[i] : in[i]).dtype == PCM_BF16 ? 2 : 0));
+        g->start[i] = (uint32_t)chunks;
+        if (in[i].count) chunks += (uint64_t)ceil_div((int64_t)((uintptr_t)in[i].data & 15) + in[i].count * size, kChunk);
         if (chunks >> 31) return false;
     }
-    l->table.start[m] = (uint32_t)chunks;
-    l->per = (uint32_t)ceil_div((int64_t)chunks, kGradBlocks);
-    l->blocks = chunks ? (uint32_t)ceil_div((int64_t)chunks, l->per) : 0;
+    g->start[m] = (uint32_t)chunks;
     return true;
 }
 
@@ -226,26 +297,29 @@ size_t grad_norm_ws_bytes(int64_t m) { return (size_t)ceil_div(m > 0 ? m : 1, Gr
 
 hipError_t launch_grad_norm(const pcm_tensor* in, const pcm_tensor* out, int m, bool clip, float max_norm, float* norm, double* parts,
                             hipStream_t s) {
+    constexpr int kMost = GradTable::kMost;
     int count = 0;
-    Launch l;
+    GradTable g;
     if (parts) {
-        for (int at = 0; at < m; at += GradTable::kMost) {
-            if (!launch_of(in + at, nullptr, m - at < GradTable::kMost ? m - at : GradTable::kMost, &l)) return hipErrorInvalidValue;
-            if (!l.blocks) continue;
-            norm_kernel<<<l.blocks, kNormThreads, 0, s>>>(l.table, l.per, parts + count);
-            count += (int)l.blocks;
+        for (int at = 0; at < m; at += kMost) {
+            if (!table_of(in + at, nullptr, m - at < kMost ? m - at : kMost, &g)) return hipErrorInvalidValue;
+            const uint32_t chunks = g.start[g.m], blocks = chunks < kGradBlocks ? chunks : kGradBlocks;
+            if (!blocks) continue;
+            norm_kernel<<<blocks, kNormThreads, 0, s>>>(g, parts + count);
+            count += (int)blocks;
         }
-        if (!clip || !count) {
+        if (!clip || count > kFewParts || !count) {
             norm_join_kernel<<<1, kNormThreads, 0, s>>>(parts, count, norm);
-            return hipGetLastError();
+            if (!clip) return hipGetLastError();
+            parts = nullptr;
         }
     }
     bool first = true;
-    for (int at = 0; at < m; at += GradTable::kMost) {
-        if (!launch_of(in + at, out ? out + at : nullptr, m - at < GradTable::kMost ? m - at : GradTable::kMost, &l))
-            return hipErrorInvalidValue;
-        if (!l.blocks) continue;
-        clip_kernel<<<l.blocks, kNormThreads, 0, s>>>(l.table, l.per, parts, count, norm, first, max_norm);
+    for (int at = 0; at < m; at += kMost) {
+        if (!table_of(in + at, out ? out + at : nullptr, m - at < kMost ? m - at : kMost, &g)) return hipErrorInvalidValue;
+        const uint32_t chunks = g.start[g.m], blocks = chunks < (1u << 22) ? chunks : (1u << 22);
+        if (!blocks) continue;
+        clip_kernel<<<blocks, kNormThreads, 0, s>>>(g, parts, count, norm, first, max_norm);
         first = false;
     }
     return hipGetLastError();
