@@ -12,7 +12,7 @@
 namespace pcm {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kGradThreads = 256;
 
 // Sum over the wavefront, on every lane.
 __device__ __forceinline__ float wave_sum(float v) {
@@ -139,7 +139,8 @@ hipError_t rows_by_type(bool bf16, bool out_bf16, const RowsArgs& g, hipStream_t
     return out_bf16 ? rows_by_slots<float, uint16_t, TO_ROWS>(g, s) : rows_by_slots<float, float, TO_ROWS>(g, s);
 }
 
-// The token's paths. A path counts where its bit is set and both of its rows are there.
+// The token's paths: those whose two rows are there, and a row to read in any case (0 for a number that is no row; a
+// token without paths reads none).
 template <int K>
 struct Paths {
     uint64_t bits;
@@ -149,114 +150,209 @@ struct Paths {
 template <int K>
 __device__ __forceinline__ Paths<K> paths_of(const MixRowsArgs& g, int64_t t) {
     Paths<K> p;
-    p.bits = g.bits[t];
+    uint64_t from = 0, to = 0;
 #pragma unroll
     for (int a = 0; a < K; ++a) {
         p.src[a] = g.src_row_of[t * K + a];
         p.tgt[a] = g.tgt_row_of[t * K + a];
+    }
+#pragma unroll
+    for (int a = 0; a < K; ++a) {
         p.has_src[a] = (uint32_t)p.src[a] < (uint32_t)g.R_src;
         p.has_tgt[a] = (uint32_t)p.tgt[a] < (uint32_t)g.R_tgt;
+        p.src[a] = p.has_src[a] ? p.src[a] : 0;
+        p.tgt[a] = p.has_tgt[a] ? p.tgt[a] : 0;
+        constexpr uint64_t kRow = ((uint64_t)1 << K) - 1;
+        from |= p.has_src[a] ? kRow << (a * K) : 0;
+#pragma unroll
+        for (int q = 0; q < K; ++q) to |= p.has_tgt[a] ? (uint64_t)1 << (q * K + a) : 0;
     }
+    p.bits = g.bits[t] & from & to;
     return p;
 }
 
-template <class IN, class OUT, int K>
+// C columns of a row in float32 registers.
+template <int C>
+struct Cols {
+    float v[C];
+};
+template <int C>
+__device__ __forceinline__ Cols<C> load_cols(const uint16_t* p) {
+    typedef uint32_t words __attribute__((ext_vector_type(C / 2)));
+    const words w = *(const words*)p;
+    Cols<C> r;
+#pragma unroll
+    for (int i = 0; i < C / 2; ++i) {
+        r.v[2 * i] = __uint_as_float(w[i] << 16);
+        r.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+    return r;
+}
+template <int C>
+__device__ __forceinline__ Cols<C> load_cols(const float* p) {
+    Cols<C> r;
+#pragma unroll
+    for (int i = 0; i < C; i += 4) {
+        const floatx4 a = *(const floatx4*)(p + i);
+        r.v[i] = a[0]; r.v[i + 1] = a[1]; r.v[i + 2] = a[2]; r.v[i + 3] = a[3];
+    }
+    return r;
+}
+template <int C>
+__device__ __forceinline__ void store_cols(uint16_t* p, const Cols<C>& x) {
+    typedef __bf16 out_t __attribute__((ext_vector_type(C)));
+    out_t y;
+#pragma unroll
+    for (int i = 0; i < C; ++i) y[i] = (__bf16)x.v[i];
+    *(out_t*)p = y;
+}
+template <int C>
+__device__ __forceinline__ void store_cols(float* p, const Cols<C>& x) {
+#pragma unroll
+    for (int i = 0; i < C; i += 4) *(floatx4*)(p + i) = floatx4{x.v[i], x.v[i + 1], x.v[i + 2], x.v[i + 3]};
+}
+
+constexpr int pow2_above(int v) { return v <= 1 ? 1 : 2 * pow2_above((v + 1) / 2); }
+
+// Sums of N values (a power of two up to 64) over the wavefront, all lanes active: lane l ends with the whole sum of value
+// l * N / 64. While there are several values a step halves them: each lane gives one half away and adds what its partner,
+// on the other side of the step's bit, gives it; then steps of one value. 63 additions for 64 values, where a sum each
+// would take 384. Bits 5 and 4: v_permlane32_swap and 16_swap exchange a half of one register with a half of another;
+// below, partners are mirrors in 16 and 8 lanes and neighbours at 2 and 1 (DPP), each of which crosses its bit.
+__device__ __forceinline__ float dpp_f32(float v, const int bit) {
+    const int i = __float_as_int(v);
+    switch (bit) {
+        case 3: return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0x140, 0xF, 0xF, true));   // row_mirror
+        case 2: return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0x141, 0xF, 0xF, true));   // row_half_mirror
+        case 1: return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0x4E, 0xF, 0xF, true));    // lane ^ 2
+        default: return __int_as_float(__builtin_amdgcn_update_dpp(0, i, 0xB1, 0xF, 0xF, true));   // lane ^ 1
+    }
+}
+__device__ __forceinline__ float joined32(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float joined16(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <int N, int BIT = 5>
+__device__ __forceinline__ float wave_sums(float (&v)[N]) {
+    constexpr int H = N > 1 ? N / 2 : 1;   // values left after the step of this bit
+    float w[H];
+    const bool upper = (threadIdx.x >> BIT) & 1;
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+        const float a = v[i], b = N > 1 ? v[i + H] : v[i];
+        if constexpr (BIT == 5) w[i] = joined32(a, b);
+        else if constexpr (BIT == 4) w[i] = joined16(a, b);
+        else w[i] = (upper ? b : a) + dpp_f32(upper ? a : b, BIT);
+    }
+    if constexpr (BIT == 0) return w[0];
+    else return wave_sums<H, BIT - 1>(w);
+}
+
+// BACK: the gradient by u alone, which is the mix of dz from the targets to the sources.
+template <class IN, class OUT, int K, bool BACK>
 __global__ __launch_bounds__(kThreads) void mix_rows_kernel(MixRowsArgs g) {
-    const IN* __restrict__ u = (const IN*)g.u;
-    OUT* __restrict__ z = (OUT*)g.out;
+    const IN* __restrict__ in = (const IN*)(BACK ? g.dz : g.u);
+    OUT* __restrict__ out = (OUT*)g.out;
     for (int64_t t = blockIdx.x; t < g.T; t += gridDim.x) {
         const Paths<K> p = paths_of<K>(g, t);
-        const float* beta = g.beta + t * K * K;
+        float beta[K * K];
+#pragma unroll
+        for (int i = 0; i < K * K; ++i) beta[i] = g.beta[t * K * K + i];
         for (int c = (blockIdx.y * blockDim.x + threadIdx.x) * 8; c < g.F; c += gridDim.y * blockDim.x * 8) {
             Eight v[K];
+            if (p.bits)
 #pragma unroll
-            for (int a = 0; a < K; ++a)
-                if (p.has_src[a]) v[a] = load8(u + (int64_t)p.src[a] * g.F + c);
+                for (int a = 0; a < K; ++a) v[a] = load8(in + (int64_t)(BACK ? p.tgt[a] : p.src[a]) * g.F + c);
 #pragma unroll
             for (int b = 0; b < K; ++b) {
-                if (!p.has_tgt[b]) continue;
+                if (!(BACK ? p.has_src[b] : p.has_tgt[b])) continue;
                 Eight s{};
 #pragma unroll
-                for (int a = 0; a < K; ++a)
-                    if (p.has_src[a] && ((p.bits >> (a * K + b)) & 1)) {
-                        const float w = beta[a * K + b];
+                for (int a = 0; a < K; ++a) {
+                    const int i = BACK ? b * K + a : a * K + b;
+                    if ((p.bits >> i) & 1)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) s.v[i] = fmaf(w, v[a].v[i], s.v[i]);
-                    }
-                store8(z + (int64_t)p.tgt[b] * g.F + c, s);
+                        for (int q = 0; q < 8; ++q) s.v[q] = fmaf(beta[i], v[a].v[q], s.v[q]);
+                }
+                store8(out + (int64_t)(BACK ? p.src[b] : p.tgt[b]) * g.F + c, s);
             }
         }
     }
 }
 
-// A thread takes four columns: the K rows of both sides and K * K sums for dbeta stay in registers.
-struct Four {
-    float v[4];
-};
-__device__ __forceinline__ Four load4(const uint16_t* p) {
-    typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
-    const uintx2 w = *(const uintx2*)p;
-    return Four{{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u), __uint_as_float(w[1] << 16),
-                 __uint_as_float(w[1] & 0xFFFF0000u)}};
-}
-__device__ __forceinline__ Four load4(const float* p) {
-    const floatx4 a = *(const floatx4*)p;
-    return Four{{a[0], a[1], a[2], a[3]}};
-}
-__device__ __forceinline__ void store4(uint16_t* p, const Four& x) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    *(bf16x4*)p = bf16x4{(__bf16)x.v[0], (__bf16)x.v[1], (__bf16)x.v[2], (__bf16)x.v[3]};
-}
-__device__ __forceinline__ void store4(float* p, const Four& x) { *(floatx4*)p = floatx4{x.v[0], x.v[1], x.v[2], x.v[3]}; }
-
-template <class IN, class OUT, int K>
-__global__ __launch_bounds__(kThreads) void mix_rows_grad_kernel(MixRowsArgs g) {
-    __shared__ float part[kThreads / 64][K * K];
+// The waves of a workgroup are shared by its tokens, `per` to each; all lanes of a wave stay active (past the last column
+// on the last ones again, as zeros), so that the sums cross the whole wave.
+template <class IN, class OUT, int K, int C>
+__global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs g, int per) {
+    constexpr int N = pow2_above(K * K);
+    __shared__ float part[kGradThreads / 64][N];
     const IN* __restrict__ u = (const IN*)g.u;
     const IN* __restrict__ dz = (const IN*)g.dz;
     OUT* __restrict__ du = (OUT*)g.out;
-    for (int64_t t = blockIdx.x; t < g.T; t += gridDim.x) {
-        const Paths<K> p = paths_of<K>(g, t);
-        const float* beta = g.beta + t * K * K;
-        float dot[K * K];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x / 64, tokens = waves / per, mine = wave / per, sub = wave - mine * per;
+    for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < g.T; t0 += (int64_t)gridDim.x * tokens) {
+        const int64_t t = t0 + mine;
+        float dot[N];
 #pragma unroll
-        for (int i = 0; i < K * K; ++i) dot[i] = 0.0f;
-        for (int c = threadIdx.x * 4; c < g.F; c += blockDim.x * 4) {
-            Four v[K], d[K];
+        for (int i = 0; i < N; ++i) dot[i] = 0.0f;
+        if (t < g.T) {
+            const Paths<K> p = paths_of<K>(g, t);
+            float beta[K * K];
 #pragma unroll
-            for (int a = 0; a < K; ++a) {
-                if (g.dbeta && p.has_src[a]) v[a] = load4(u + (int64_t)p.src[a] * g.F + c);
-                if (p.has_tgt[a]) d[a] = load4(dz + (int64_t)p.tgt[a] * g.F + c);
-            }
+            for (int i = 0; i < K * K; ++i) beta[i] = g.beta[t * K * K + i];
+            for (int c0 = sub * 64 * C; c0 < g.F; c0 += per * 64 * C) {
+                const int at = c0 + lane * C, c = min(at, g.F - C);
+                Cols<C> v[K], d[K];
+                if (p.bits) {
 #pragma unroll
-            for (int a = 0; a < K; ++a) {
-                if (!p.has_src[a]) continue;
-                Four s{};
-#pragma unroll
-                for (int b = 0; b < K; ++b)
-                    if (p.has_tgt[b] && ((p.bits >> (a * K + b)) & 1)) {
-                        const float w = beta[a * K + b];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            s.v[i] = fmaf(w, d[b].v[i], s.v[i]);
-                            if (g.dbeta) dot[a * K + b] = fmaf(v[a].v[i], d[b].v[i], dot[a * K + b]);
-                        }
+                    for (int a = 0; a < K; ++a) {
+                        v[a] = load_cols<C>(u + (int64_t)p.src[a] * g.F + c);
+                        d[a] = load_cols<C>(dz + (int64_t)p.tgt[a] * g.F + c);
                     }
-                if (du) store4(du + (int64_t)p.src[a] * g.F + c, s);
+                }
+                if (c0 + 64 * C > g.F) {
+#pragma unroll
+                    for (int a = 0; a < K; ++a)
+#pragma unroll
+                        for (int i = 0; i < C; ++i) {
+                            v[a].v[i] = at < g.F ? v[a].v[i] : 0.0f;
+                            d[a].v[i] = at < g.F ? d[a].v[i] : 0.0f;
+                        }
+                }
+#pragma unroll
+                for (int a = 0; a < K; ++a) {
+                    Cols<C> s{};
+#pragma unroll
+                    for (int b = 0; b < K; ++b)
+                        if ((p.bits >> (a * K + b)) & 1) {
+#pragma unroll
+                            for (int i = 0; i < C; ++i) {
+                                s.v[i] = fmaf(beta[a * K + b], d[b].v[i], s.v[i]);
+                                dot[a * K + b] = fmaf(v[a].v[i], d[b].v[i], dot[a * K + b]);
+                            }
+                        }
+                    if (du && p.has_src[a] && at < g.F) store_cols<C>(du + (int64_t)p.src[a] * g.F + at, s);
+                }
             }
         }
-        if (!g.dbeta) continue;
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-        for (int i = 0; i < K * K; ++i) {
-            const float s = wave_sum(dot[i]);
-            if (lane == 0) part[wave][i] = s;
+        const float sum = wave_sums<N>(dot);
+        constexpr int kLanes = 64 / N;
+        const int i = lane / kLanes;
+        if (per == 1) {
+            if (t < g.T && lane % kLanes == 0 && i < K * K) g.dbeta[t * K * K + i] = sum;
+            continue;
         }
+        if (lane % kLanes == 0) part[wave][i] = sum;
         __syncthreads();
-        if (threadIdx.x < K * K) {
+        if (sub == 0 && t < g.T && lane < K * K) {
             float s = 0.0f;
-            for (int q = 0; q < (int)blockDim.x / 64; ++q) s += part[q][threadIdx.x];
-            g.dbeta[t * K * K + threadIdx.x] = s;
+            for (int q = 0; q < per; ++q) s += part[wave + q][lane];
+            g.dbeta[t * K * K + lane] = s;
         }
         __syncthreads();
     }
@@ -264,15 +360,22 @@ __global__ __launch_bounds__(kThreads) void mix_rows_grad_kernel(MixRowsArgs g) 
 
 template <class IN, class OUT, int K>
 hipError_t mix_sized(bool grad, const MixRowsArgs& g, hipStream_t s) {
-    const unsigned blocks = (unsigned)(g.T < (1 << 20) ? g.T : (1 << 20));
-    const int64_t chunks = grad ? g.F / 4 : g.F / 8;
-    const int threads = (int)(chunks >= kThreads ? kThreads : align_up(chunks, 64));
-    if (grad) {
-        mix_rows_grad_kernel<IN, OUT, K><<<dim3(blocks), threads, 0, s>>>(g);
-    } else {
-        const int64_t split = ceil_div(chunks, threads);
-        mix_rows_kernel<IN, OUT, K><<<dim3(blocks, (unsigned)(split < 64 ? split : 64)), threads, 0, s>>>(g);
+    if (grad && g.dbeta) {
+        // Waves for a token: steps of 64 C columns, up to four to a wave.
+        constexpr int C = K > 4 ? 4 : 8;
+        const int64_t steps = ceil_div(g.F, 64 * C);
+        const int per = steps <= 4 ? 1 : steps <= 8 ? 2 : 4, tokens = kGradThreads / 64 / per;
+        const int64_t blocks = ceil_div(g.T, tokens);
+        mix_rows_grad_kernel<IN, OUT, K, C><<<dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20))), kGradThreads, 0, s>>>(g, per);
+        return hipGetLastError();
     }
+    const unsigned blocks = (unsigned)(g.T < (1 << 20) ? g.T : (1 << 20));
+    const int64_t chunks = g.F / 8;
+    const int threads = (int)(chunks >= kThreads ? kThreads : align_up(chunks, 64));
+    const int64_t split = ceil_div(chunks, threads);
+    const dim3 grid(blocks, (unsigned)(split < 64 ? split : 64));
+    if (grad) mix_rows_kernel<IN, OUT, K, true><<<grid, threads, 0, s>>>(g);
+    else mix_rows_kernel<IN, OUT, K, false><<<grid, threads, 0, s>>>(g);
     return hipGetLastError();
 }
 
