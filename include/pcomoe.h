@@ -395,7 +395,7 @@ pcm_status pcm_grouped_gemm_fp8(pcm_dtype out_dtype, const uint8_t* x, const flo
 /* ---------------------------------------------------------------- training around the experts' products
  * What a training step does between the products above, with its gradients. `dtype` is that of the inputs,
  * `out_dtype` that of the result, each PCM_F32 or PCM_BF16; computed in float32, rounded once, to nearest even.
- * Limits: widths (H, F) multiples of 16, at most 2^31 - 128; k <= 8; n <= 256; T and R below 2^30. Outputs must not
+ * Limits: widths (H, F) multiples of 16, at most 2^28; k <= 8; n <= 256; T and R below 2^30. Outputs must not
  * overlap inputs (but for the gradients clipped in place). Deterministic. */
 
 /* Rows of tokens. row_of [T,k] i32: the row of pair (t, a), as in pcm_paths; a number outside [offsets[0],

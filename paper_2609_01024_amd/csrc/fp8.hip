@@ -6,7 +6,7 @@
 // 2 x 1408 41 us (5.7), 64 weights of 2048 x 1024 with their transposes 104 us (5.1 of the 5.1 TB/s that a
 // copy has). The product: 8192^3 2060 TF into bf16; 8 experts of 14336 x 4096 with 8192 rows 560-580 us; 256
 // of 2048 x 7168 with one row each 345-360 us (weights at 6.7-7 TB/s).
-#include "eight.h"
+#include "columns.h"
 #include "grouped.h"
 
 namespace pcm {

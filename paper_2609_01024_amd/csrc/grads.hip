@@ -1,7 +1,7 @@
 // The router's gradient from those of the weights it gave, and the norm over all gradients with clipping.
 #include "pcomoe.h"
 
-#include "eight.h"
+#include "columns.h"
 
 namespace pcm {
 namespace {

@@ -302,6 +302,7 @@ struct RowsArgs {
     int64_t T, R;
     int k, H, n;
     int accumulate;           // combine: add into out
+    int parts;                // set by the launch: workgroups to a token's columns
 };
 hipError_t launch_rows(bool to_rows, bool bf16, bool out_bf16, const RowsArgs& g, hipStream_t s);
 // The mix along a token's paths and its gradient.
@@ -316,6 +317,7 @@ struct MixRowsArgs {
     const int32_t* tgt_row_of;
     int64_t T, R_src, R_tgt;
     int k, F;
+    int parts;                // set by the launch, as above
 };
 hipError_t launch_mix_rows(bool grad, bool bf16, bool out_bf16, const MixRowsArgs& g, hipStream_t s);
 // u = SiLU(gate) * up, or, with du, the gradient by gate_up (swiglu.hip).

@@ -81,10 +81,12 @@ bool grouped_rows(const int32_t* offsets, const int32_t* row_token, int64_t T, i
 }
 
 // Training around the products: sizes, then what the calls on rows share.
+constexpr int kMaxRowWidth = 1 << 28;   // a column's offset in bytes, and the next step's column, fit in 32 bits
 pcm_status check_rows(int64_t T, int64_t R, int k, int H, int n) {
     const pcm_status st = check_grouped(T, R, H, 16, n);
     if (st != PCM_OK) return st;
     if (k < 1) return PCM_ERR_ARG;
+    if (H > kMaxRowWidth) return PCM_ERR_UNSUPPORTED;
     return k > kMaxK ? PCM_ERR_UNSUPPORTED : PCM_OK;
 }
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }   // any element of an array of 32-bit numbers

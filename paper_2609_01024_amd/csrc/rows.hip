@@ -7,210 +7,12 @@
 //   its gradient    du[src_a] = sum_b beta_ab dz[tgt_b],   dbeta_ab = <dz[tgt_b], u[src_a]>
 // All are bound by memory. A workgroup takes a token: the token's row numbers and weights are scalars there, and what
 // the rows of a token share (its own row, or the sum) is read or written once. Sums are float32, slots ascending.
-#include "eight.h"
+#include "columns.h"
 
 namespace pcm {
 namespace {
 
 constexpr int kThreads = 256, kGradThreads = 256;
-
-// Sum over the wavefront, on every lane.
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
-
-// Rows [first, first + count) of the groups, inside [0, R).
-__device__ __forceinline__ void held_rows(const int32_t* offsets, int n, int64_t R, int& first, int& count) {
-    first = 0;
-    count = (int)R;
-    if (!offsets) return;
-    const int lo = min(max(offsets[0], 0), (int)R), hi = min(max(offsets[n], lo), (int)R);
-    first = lo;
-    count = hi - lo;
-}
-
-// TO_ROWS: dispatch and the combine's gradient, from `tokens` to the rows of out; otherwise combine and the dispatch's
-// gradient, from `rows` to the tokens of out. DOT: dweights too, from both.
-template <class IN, class OUT, int KK, bool TO_ROWS, bool DOT>
-__global__ __launch_bounds__(kThreads) void rows_kernel(RowsArgs g) {
-    __shared__ float part[KK][kThreads / 64];
-    const IN* __restrict__ tokens = (const IN*)g.tokens;
-    const IN* __restrict__ rows = (const IN*)g.rows;
-    OUT* __restrict__ out = (OUT*)g.out;
-    int first, count;
-    held_rows(g.offsets, g.n, g.R, first, count);
-    for (int64_t t = blockIdx.x; t < g.T; t += gridDim.x) {
-        int r[KK];
-        float w[KK], dot[KK];
-        bool on[KK];
-#pragma unroll
-        for (int a = 0; a < KK; ++a) {
-            r[a] = a < g.k ? g.row_of[t * g.k + a] : -1;
-            w[a] = g.weights && a < g.k ? g.weights[t * g.k + a] : 1.0f;
-            dot[a] = 0.0f;
-            on[a] = a < g.k && (uint32_t)r[a] - (uint32_t)first < (uint32_t)count;
-        }
-        for (int c = (blockIdx.y * blockDim.x + threadIdx.x) * 8; c < g.H; c += gridDim.y * blockDim.x * 8) {
-            Eight x{}, v[KK];
-            if (TO_ROWS || DOT) x = load8(tokens + t * g.H + c);
-            if (!TO_ROWS || DOT) {
-#pragma unroll
-                for (int a = 0; a < KK; ++a)
-                    if (on[a]) v[a] = load8(rows + (int64_t)r[a] * g.H + c);
-            }
-            if constexpr (DOT) {
-#pragma unroll
-                for (int a = 0; a < KK; ++a)
-                    if (on[a]) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) dot[a] = fmaf(v[a].v[i], x.v[i], dot[a]);
-                    }
-            }
-            if (!out) continue;
-            if constexpr (TO_ROWS) {
-#pragma unroll
-                for (int a = 0; a < KK; ++a)
-                    if (on[a]) {
-                        Eight y;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) y.v[i] = w[a] * x.v[i];
-                        store8(out + (int64_t)r[a] * g.H + c, y);
-                    }
-            } else {
-                Eight y{};
-                if (g.accumulate) y = load8(out + t * g.H + c);
-                Eight s{};
-#pragma unroll
-                for (int a = 0; a < KK; ++a)
-                    if (on[a]) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) s.v[i] = fmaf(w[a], v[a].v[i], s.v[i]);
-                    }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y.v[i] += s.v[i];
-                store8(out + t * g.H + c, y);
-            }
-        }
-        if constexpr (DOT) {
-            const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-            for (int a = 0; a < KK; ++a) {
-                const float s = wave_sum(dot[a]);
-                if (lane == 0) part[a][wave] = s;
-            }
-            __syncthreads();
-            if (threadIdx.x < (unsigned)g.k) {
-                float s = 0.0f;
-                for (int q = 0; q < (int)blockDim.x / 64; ++q) s += part[threadIdx.x][q];
-                g.dweights[t * g.k + threadIdx.x] = s;
-            }
-            __syncthreads();
-        }
-    }
-}
-
-template <class IN, class OUT, int KK, bool TO_ROWS>
-hipError_t rows_by_dot(const RowsArgs& g, hipStream_t s) {
-    const int64_t chunks = g.H / 8;
-    const int threads = (int)(chunks >= kThreads ? kThreads : align_up(chunks, 64));
-    const unsigned blocks = (unsigned)(g.T < (1 << 20) ? g.T : (1 << 20));
-    if (g.dweights) {
-        rows_kernel<IN, OUT, KK, TO_ROWS, true><<<dim3(blocks), threads, 0, s>>>(g);
-    } else {
-        const int64_t split = ceil_div(chunks, threads);
-        rows_kernel<IN, OUT, KK, TO_ROWS, false><<<dim3(blocks, (unsigned)(split < 64 ? split : 64)), threads, 0, s>>>(g);
-    }
-    return hipGetLastError();
-}
-
-template <class IN, class OUT, bool TO_ROWS>
-hipError_t rows_by_slots(const RowsArgs& g, hipStream_t s) {
-    if (g.k <= 1) return rows_by_dot<IN, OUT, 1, TO_ROWS>(g, s);
-    if (g.k <= 2) return rows_by_dot<IN, OUT, 2, TO_ROWS>(g, s);
-    if (g.k <= 4) return rows_by_dot<IN, OUT, 4, TO_ROWS>(g, s);
-    return rows_by_dot<IN, OUT, 8, TO_ROWS>(g, s);
-}
-
-template <bool TO_ROWS>
-hipError_t rows_by_type(bool bf16, bool out_bf16, const RowsArgs& g, hipStream_t s) {
-    if (bf16) return out_bf16 ? rows_by_slots<uint16_t, uint16_t, TO_ROWS>(g, s) : rows_by_slots<uint16_t, float, TO_ROWS>(g, s);
-    return out_bf16 ? rows_by_slots<float, uint16_t, TO_ROWS>(g, s) : rows_by_slots<float, float, TO_ROWS>(g, s);
-}
-
-// The token's paths: those whose two rows are there, and a row to read in any case (0 for a number that is no row; a
-// token without paths reads none).
-template <int K>
-struct Paths {
-    uint64_t bits;
-    int src[K], tgt[K];
-    bool has_src[K], has_tgt[K];
-};
-template <int K>
-__device__ __forceinline__ Paths<K> paths_of(const MixRowsArgs& g, int64_t t) {
-    Paths<K> p;
-    uint64_t from = 0, to = 0;
-#pragma unroll
-    for (int a = 0; a < K; ++a) {
-        p.src[a] = g.src_row_of[t * K + a];
-        p.tgt[a] = g.tgt_row_of[t * K + a];
-    }
-#pragma unroll
-    for (int a = 0; a < K; ++a) {
-        p.has_src[a] = (uint32_t)p.src[a] < (uint32_t)g.R_src;
-        p.has_tgt[a] = (uint32_t)p.tgt[a] < (uint32_t)g.R_tgt;
-        p.src[a] = p.has_src[a] ? p.src[a] : 0;
-        p.tgt[a] = p.has_tgt[a] ? p.tgt[a] : 0;
-        constexpr uint64_t kRow = ((uint64_t)1 << K) - 1;
-        from |= p.has_src[a] ? kRow << (a * K) : 0;
-#pragma unroll
-        for (int q = 0; q < K; ++q) to |= p.has_tgt[a] ? (uint64_t)1 << (q * K + a) : 0;
-    }
-    p.bits = g.bits[t] & from & to;
-    return p;
-}
-
-// C columns of a row in float32 registers.
-template <int C>
-struct Cols {
-    float v[C];
-};
-template <int C>
-__device__ __forceinline__ Cols<C> load_cols(const uint16_t* p) {
-    typedef uint32_t words __attribute__((ext_vector_type(C / 2)));
-    const words w = *(const words*)p;
-    Cols<C> r;
-#pragma unroll
-    for (int i = 0; i < C / 2; ++i) {
-        r.v[2 * i] = __uint_as_float(w[i] << 16);
-        r.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-    return r;
-}
-template <int C>
-__device__ __forceinline__ Cols<C> load_cols(const float* p) {
-    Cols<C> r;
-#pragma unroll
-    for (int i = 0; i < C; i += 4) {
-        const floatx4 a = *(const floatx4*)(p + i);
-        r.v[i] = a[0]; r.v[i + 1] = a[1]; r.v[i + 2] = a[2]; r.v[i + 3] = a[3];
-    }
-    return r;
-}
-template <int C>
-__device__ __forceinline__ void store_cols(uint16_t* p, const Cols<C>& x) {
-    typedef __bf16 out_t __attribute__((ext_vector_type(C)));
-    out_t y;
-#pragma unroll
-    for (int i = 0; i < C; ++i) y[i] = (__bf16)x.v[i];
-    *(out_t*)p = y;
-}
-template <int C>
-__device__ __forceinline__ void store_cols(float* p, const Cols<C>& x) {
-#pragma unroll
-    for (int i = 0; i < C; i += 4) *(floatx4*)(p + i) = floatx4{x.v[i], x.v[i + 1], x.v[i + 2], x.v[i + 3]};
-}
 
 constexpr int pow2_above(int v) { return v <= 1 ? 1 : 2 * pow2_above((v + 1) / 2); }
 
@@ -252,33 +54,218 @@ __device__ __forceinline__ float wave_sums(float (&v)[N]) {
     else return wave_sums<H, BIT - 1>(w);
 }
 
+// Scalar loads of what a token's slots or paths have (the address is the same on every lane; nothing writes there while the
+// kernel runs). All of them are on their way before the first wait: read under a branch or by vector loads, each waited for
+// the one before (8192 tokens of 8 rows, combine 74 us, 56 with one wait).
+template <class T>
+using Scalar = const __attribute__((address_space(4))) T*;
+template <class T>
+__device__ __forceinline__ Scalar<T> scalar(const T* p) { return (Scalar<T>)p; }
+
+// Rows [first, first + count) of the groups, inside [0, R).
+__device__ __forceinline__ void held_rows(const int32_t* offsets, int n, int64_t R, int& first, int& count) {
+    first = 0;
+    count = (int)R;
+    if (!offsets) return;
+    const int lo = min(max(scalar(offsets)[0], 0), (int)R), hi = min(max(scalar(offsets)[n], lo), (int)R);
+    first = lo;
+    count = hi - lo;
+}
+
+// Element c of the row that starts at element `row` of p: a scalar address and 32 bits of offset.
+template <class T>
+__device__ __forceinline__ T* column(T* __restrict__ p, int64_t row, uint32_t c) {
+    return (T*)((char*)(p + row) + c * (uint32_t)sizeof(T));
+}
+
+// TO_ROWS: dispatch and the combine's gradient, from `tokens` to the rows of out; otherwise combine and the dispatch's
+// gradient, from `rows` to the tokens of out. DOT: dweights too, from both.
+template <class IN, class OUT, int KK, bool TO_ROWS, bool DOT, bool STREAM>
+__global__ __launch_bounds__(kThreads) void rows_kernel(RowsArgs g) {
+    constexpr int C = kCols<IN, OUT>;
+    __shared__ float part[kThreads / 64][KK];
+    const IN* __restrict__ tokens = (const IN*)g.tokens;
+    const IN* __restrict__ rows = (const IN*)g.rows;
+    OUT* __restrict__ out = (OUT*)g.out;
+    for (int64_t item = blockIdx.x; item < g.T * g.parts; item += gridDim.x) {
+        const int64_t t = g.parts == 1 ? item : item / g.parts;
+        const int part0 = (int)(item - t * g.parts);
+        int64_t r[KK];
+        float w[KK], dot[KK];
+        int row[KK];
+#pragma unroll
+        for (int a = 0; a < KK; ++a) {
+            const int64_t slot = t * g.k + min(a, g.k - 1);
+            row[a] = scalar(g.row_of)[slot];
+            w[a] = 1.0f;
+            if (g.weights) w[a] = scalar(g.weights)[slot];
+            dot[a] = 0.0f;
+        }
+        int first, count;
+        held_rows(g.offsets, g.n, g.R, first, count);
+        uint32_t held = 0;
+#pragma unroll
+        for (int a = 0; a < KK; ++a) {
+            const bool on = a < g.k && (uint32_t)row[a] - (uint32_t)first < (uint32_t)count;
+            held |= on ? 1u << a : 0u;
+            r[a] = (int64_t)(on ? row[a] : first) * g.H;   // a row to read in any case, where there are any
+        }
+        for (int c = (part0 * blockDim.x + threadIdx.x) * C; c < g.H; c += g.parts * blockDim.x * C) {
+            Raw<IN, C> x, v[KK];
+            if (TO_ROWS || DOT) x.load(column(tokens, t * g.H, c));
+            if ((!TO_ROWS || DOT) && held) {
+#pragma unroll
+                for (int a = 0; a < KK; ++a) read<STREAM>(v[a], column(rows, r[a], c));
+            }
+            Raw<float, C> before;
+            if (!TO_ROWS && g.accumulate) before.load(column((const float*)g.out, t * g.H, c));
+            if constexpr (DOT) {
+#pragma unroll
+                for (int a = 0; a < KK; ++a)
+                    if ((held >> a) & 1) {
+#pragma unroll
+                        for (int i = 0; i < C; ++i) dot[a] = fmaf(v[a].at(i), x.at(i), dot[a]);
+                    }
+            }
+            if (!out) continue;
+            Cols<C> y{};
+            if constexpr (TO_ROWS) {
+#pragma unroll
+                for (int a = 0; a < KK; ++a)
+                    if ((held >> a) & 1) {
+#pragma unroll
+                        for (int i = 0; i < C; ++i) y.v[i] = w[a] * x.at(i);
+                        store_cols<C>(column(out, r[a], c), y);
+                    }
+            } else {
+#pragma unroll
+                for (int a = 0; a < KK; ++a)
+                    if ((held >> a) & 1) {
+#pragma unroll
+                        for (int i = 0; i < C; ++i) y.v[i] = fmaf(w[a], v[a].at(i), y.v[i]);
+                    }
+                if (g.accumulate)
+#pragma unroll
+                    for (int i = 0; i < C; ++i) y.v[i] += before.at(i);
+                store_cols<C>(column(out, t * g.H, c), y);
+            }
+        }
+        if constexpr (DOT) {
+            const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+            const float sum = wave_sums<KK>(dot);
+            if (lane % (64 / KK) == 0) part[wave][lane / (64 / KK)] = sum;
+            __syncthreads();
+            if (threadIdx.x < (unsigned)g.k) {
+                float s = 0.0f;
+                for (int q = 0; q < (int)blockDim.x / 64; ++q) s += part[q][threadIdx.x];
+                g.dweights[t * g.k + threadIdx.x] = s;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+constexpr int64_t kMostBlocks = 1 << 22;
+
+template <class IN, class OUT, int KK, bool TO_ROWS, bool STREAM>
+hipError_t rows_by_dot(RowsArgs g, hipStream_t s) {
+    const int64_t chunks = g.H / kCols<IN, OUT>;
+    const int threads = (int)(chunks >= kThreads ? kThreads : align_up(chunks, 64));
+    g.parts = g.dweights ? 1 : (int)ceil_div(chunks, threads);
+    const int64_t items = g.T * g.parts;
+    const unsigned blocks = (unsigned)(items < kMostBlocks ? items : kMostBlocks);
+    if (g.dweights) rows_kernel<IN, OUT, KK, TO_ROWS, true, STREAM><<<dim3(blocks), threads, 0, s>>>(g);
+    else rows_kernel<IN, OUT, KK, TO_ROWS, false, STREAM><<<dim3(blocks), threads, 0, s>>>(g);
+    return hipGetLastError();
+}
+
+template <class IN, class OUT, bool TO_ROWS, bool STREAM>
+hipError_t rows_by_slots(const RowsArgs& g, hipStream_t s) {
+    if (g.k <= 1) return rows_by_dot<IN, OUT, 1, TO_ROWS, STREAM>(g, s);
+    if (g.k <= 2) return rows_by_dot<IN, OUT, 2, TO_ROWS, STREAM>(g, s);
+    if (g.k <= 4) return rows_by_dot<IN, OUT, 4, TO_ROWS, STREAM>(g, s);
+    return rows_by_dot<IN, OUT, 8, TO_ROWS, STREAM>(g, s);
+}
+
+template <class IN, class OUT, bool TO_ROWS>
+hipError_t rows_by_size(const RowsArgs& g, hipStream_t s) {
+    return streamed(g.R * g.H * (int64_t)sizeof(IN)) ? rows_by_slots<IN, OUT, TO_ROWS, true>(g, s)
+                                                     : rows_by_slots<IN, OUT, TO_ROWS, false>(g, s);
+}
+
+template <bool TO_ROWS>
+hipError_t rows_by_type(bool bf16, bool out_bf16, const RowsArgs& g, hipStream_t s) {
+    if (bf16) return out_bf16 ? rows_by_size<uint16_t, uint16_t, TO_ROWS>(g, s) : rows_by_size<uint16_t, float, TO_ROWS>(g, s);
+    return out_bf16 ? rows_by_size<float, uint16_t, TO_ROWS>(g, s) : rows_by_size<float, float, TO_ROWS>(g, s);
+}
+
+// The token's paths: those whose two rows are there, and a row to read in any case (0 for a number that is no row; a
+// token without paths reads none).
+template <int K>
+struct Paths {
+    uint64_t bits;
+    uint32_t srcs, tgts;     // which slots have rows
+    int src[K], tgt[K];
+    Scalar<float> beta;
+};
+template <int K>
+__device__ __forceinline__ Paths<K> paths_of(const MixRowsArgs& g, int64_t t) {
+    Paths<K> p;
+    p.beta = scalar(g.beta) + t * (K * K);
+    p.bits = scalar(g.bits)[t];
+#pragma unroll
+    for (int a = 0; a < K; ++a) {
+        p.src[a] = scalar(g.src_row_of)[t * K + a];
+        p.tgt[a] = scalar(g.tgt_row_of)[t * K + a];
+    }
+    p.srcs = p.tgts = 0;
+    uint64_t from = 0, to = 0;
+    constexpr uint64_t kRow = ((uint64_t)1 << K) - 1;
+#pragma unroll
+    for (int a = 0; a < K; ++a) {
+        const bool s = (uint32_t)p.src[a] < (uint32_t)g.R_src, d = (uint32_t)p.tgt[a] < (uint32_t)g.R_tgt;
+        p.srcs |= s ? 1u << a : 0u;
+        p.tgts |= d ? 1u << a : 0u;
+        p.src[a] = s ? p.src[a] : 0;
+        p.tgt[a] = d ? p.tgt[a] : 0;
+        from |= s ? kRow << (a * K) : 0;
+    }
+#pragma unroll
+    for (int a = 0; a < K; ++a) to |= (uint64_t)p.tgts << (a * K);
+    p.bits &= from & to;
+    return p;
+}
+
 // BACK: the gradient by u alone, which is the mix of dz from the targets to the sources.
-template <class IN, class OUT, int K, bool BACK>
+template <class IN, class OUT, int K, bool BACK, bool STREAM>
 __global__ __launch_bounds__(kThreads) void mix_rows_kernel(MixRowsArgs g) {
+    constexpr int C = kCols<IN, OUT>;
     const IN* __restrict__ in = (const IN*)(BACK ? g.dz : g.u);
     OUT* __restrict__ out = (OUT*)g.out;
-    for (int64_t t = blockIdx.x; t < g.T; t += gridDim.x) {
+    for (int64_t item = blockIdx.x; item < g.T * g.parts; item += gridDim.x) {
+        const int64_t t = g.parts == 1 ? item : item / g.parts;
+        const int part0 = (int)(item - t * g.parts);
         const Paths<K> p = paths_of<K>(g, t);
-        float beta[K * K];
+        for (int c = (part0 * blockDim.x + threadIdx.x) * C; c < g.F; c += g.parts * blockDim.x * C) {
+            Raw<IN, C> v[K];
+            if (p.bits) {
 #pragma unroll
-        for (int i = 0; i < K * K; ++i) beta[i] = g.beta[t * K * K + i];
-        for (int c = (blockIdx.y * blockDim.x + threadIdx.x) * 8; c < g.F; c += gridDim.y * blockDim.x * 8) {
-            Eight v[K];
-            if (p.bits)
-#pragma unroll
-                for (int a = 0; a < K; ++a) v[a] = load8(in + (int64_t)(BACK ? p.tgt[a] : p.src[a]) * g.F + c);
+                for (int a = 0; a < K; ++a) read<STREAM>(v[a], column(in, (int64_t)(BACK ? p.tgt[a] : p.src[a]) * g.F, c));
+            }
 #pragma unroll
             for (int b = 0; b < K; ++b) {
-                if (!(BACK ? p.has_src[b] : p.has_tgt[b])) continue;
-                Eight s{};
+                if (!(((BACK ? p.srcs : p.tgts) >> b) & 1)) continue;
+                Cols<C> s{};
 #pragma unroll
                 for (int a = 0; a < K; ++a) {
                     const int i = BACK ? b * K + a : a * K + b;
-                    if ((p.bits >> i) & 1)
+                    if ((p.bits >> i) & 1) {
+                        const float w = p.beta[i];
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) s.v[q] = fmaf(beta[i], v[a].v[q], s.v[q]);
+                        for (int q = 0; q < C; ++q) s.v[q] = fmaf(w, v[a].at(q), s.v[q]);
+                    }
                 }
-                store8(out + (int64_t)(BACK ? p.src[b] : p.tgt[b]) * g.F + c, s);
+                store_cols<C>(column(out, (int64_t)(BACK ? p.src[b] : p.tgt[b]) * g.F, c), s);
             }
         }
     }
@@ -286,7 +273,7 @@ __global__ __launch_bounds__(kThreads) void mix_rows_kernel(MixRowsArgs g) {
 
 // The waves of a workgroup are shared by its tokens, `per` to each; all lanes of a wave stay active (past the last column
 // on the last ones again, as zeros), so that the sums cross the whole wave.
-template <class IN, class OUT, int K, int C>
+template <class IN, class OUT, int K, int C, bool STREAM>
 __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs g, int per) {
     constexpr int N = pow2_above(K * K);
     __shared__ float part[kGradThreads / 64][N];
@@ -302,27 +289,22 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
         for (int i = 0; i < N; ++i) dot[i] = 0.0f;
         if (t < g.T) {
             const Paths<K> p = paths_of<K>(g, t);
-            float beta[K * K];
-#pragma unroll
-            for (int i = 0; i < K * K; ++i) beta[i] = g.beta[t * K * K + i];
             for (int c0 = sub * 64 * C; c0 < g.F; c0 += per * 64 * C) {
                 const int at = c0 + lane * C, c = min(at, g.F - C);
-                Cols<C> v[K], d[K];
+                Raw<IN, C> v[K], d[K];
                 if (p.bits) {
 #pragma unroll
                     for (int a = 0; a < K; ++a) {
-                        v[a] = load_cols<C>(u + (int64_t)p.src[a] * g.F + c);
-                        d[a] = load_cols<C>(dz + (int64_t)p.tgt[a] * g.F + c);
+                        read<STREAM>(v[a], column(u, (int64_t)p.src[a] * g.F, c));
+                        read<STREAM>(d[a], column(dz, (int64_t)p.tgt[a] * g.F, c));
                     }
                 }
                 if (c0 + 64 * C > g.F) {
 #pragma unroll
-                    for (int a = 0; a < K; ++a)
-#pragma unroll
-                        for (int i = 0; i < C; ++i) {
-                            v[a].v[i] = at < g.F ? v[a].v[i] : 0.0f;
-                            d[a].v[i] = at < g.F ? d[a].v[i] : 0.0f;
-                        }
+                    for (int a = 0; a < K; ++a) {
+                        v[a].zero_unless(at < g.F);
+                        d[a].zero_unless(at < g.F);
+                    }
                 }
 #pragma unroll
                 for (int a = 0; a < K; ++a) {
@@ -330,13 +312,14 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
 #pragma unroll
                     for (int b = 0; b < K; ++b)
                         if ((p.bits >> (a * K + b)) & 1) {
+                            const float w = p.beta[a * K + b];
 #pragma unroll
                             for (int i = 0; i < C; ++i) {
-                                s.v[i] = fmaf(beta[a * K + b], d[b].v[i], s.v[i]);
-                                dot[a * K + b] = fmaf(v[a].v[i], d[b].v[i], dot[a * K + b]);
+                                s.v[i] = fmaf(w, d[b].at(i), s.v[i]);
+                                dot[a * K + b] = fmaf(v[a].at(i), d[b].at(i), dot[a * K + b]);
                             }
                         }
-                    if (du && p.has_src[a] && at < g.F) store_cols<C>(du + (int64_t)p.src[a] * g.F + at, s);
+                    if (du && ((p.srcs >> a) & 1) && at < g.F) store_cols<C>(column(du, (int64_t)p.src[a] * g.F, at), s);
                 }
             }
         }
@@ -358,39 +341,46 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
     }
 }
 
-template <class IN, class OUT, int K>
-hipError_t mix_sized(bool grad, const MixRowsArgs& g, hipStream_t s) {
+template <class IN, class OUT, int K, bool STREAM>
+hipError_t mix_sized(bool grad, MixRowsArgs g, hipStream_t s) {
     if (grad && g.dbeta) {
         // Waves for a token: steps of 64 C columns, up to four to a wave.
-        constexpr int C = K > 4 ? 4 : 8;
+        constexpr int C = K > 4 ? 4 : kCols<IN, OUT>;
         const int64_t steps = ceil_div(g.F, 64 * C);
         const int per = steps <= 4 ? 1 : steps <= 8 ? 2 : 4, tokens = kGradThreads / 64 / per;
         const int64_t blocks = ceil_div(g.T, tokens);
-        mix_rows_grad_kernel<IN, OUT, K, C><<<dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20))), kGradThreads, 0, s>>>(g, per);
+        mix_rows_grad_kernel<IN, OUT, K, C, STREAM>
+            <<<dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), kGradThreads, 0, s>>>(g, per);
         return hipGetLastError();
     }
-    const unsigned blocks = (unsigned)(g.T < (1 << 20) ? g.T : (1 << 20));
-    const int64_t chunks = g.F / 8;
+    const int64_t chunks = g.F / kCols<IN, OUT>;
     const int threads = (int)(chunks >= kThreads ? kThreads : align_up(chunks, 64));
-    const int64_t split = ceil_div(chunks, threads);
-    const dim3 grid(blocks, (unsigned)(split < 64 ? split : 64));
-    if (grad) mix_rows_kernel<IN, OUT, K, true><<<grid, threads, 0, s>>>(g);
-    else mix_rows_kernel<IN, OUT, K, false><<<grid, threads, 0, s>>>(g);
+    g.parts = (int)ceil_div(chunks, threads);
+    const int64_t items = g.T * g.parts;
+    const dim3 grid((unsigned)(items < kMostBlocks ? items : kMostBlocks));
+    if (grad) mix_rows_kernel<IN, OUT, K, true, STREAM><<<grid, threads, 0, s>>>(g);
+    else mix_rows_kernel<IN, OUT, K, false, STREAM><<<grid, threads, 0, s>>>(g);
     return hipGetLastError();
 }
 
-template <class IN, class OUT>
+template <class IN, class OUT, bool STREAM>
 hipError_t mix_by_slots(bool grad, const MixRowsArgs& g, hipStream_t s) {
     switch (g.k) {
-        case 1: return mix_sized<IN, OUT, 1>(grad, g, s);
-        case 2: return mix_sized<IN, OUT, 2>(grad, g, s);
-        case 3: return mix_sized<IN, OUT, 3>(grad, g, s);
-        case 4: return mix_sized<IN, OUT, 4>(grad, g, s);
-        case 5: return mix_sized<IN, OUT, 5>(grad, g, s);
-        case 6: return mix_sized<IN, OUT, 6>(grad, g, s);
-        case 7: return mix_sized<IN, OUT, 7>(grad, g, s);
-        default: return mix_sized<IN, OUT, 8>(grad, g, s);
+        case 1: return mix_sized<IN, OUT, 1, STREAM>(grad, g, s);
+        case 2: return mix_sized<IN, OUT, 2, STREAM>(grad, g, s);
+        case 3: return mix_sized<IN, OUT, 3, STREAM>(grad, g, s);
+        case 4: return mix_sized<IN, OUT, 4, STREAM>(grad, g, s);
+        case 5: return mix_sized<IN, OUT, 5, STREAM>(grad, g, s);
+        case 6: return mix_sized<IN, OUT, 6, STREAM>(grad, g, s);
+        case 7: return mix_sized<IN, OUT, 7, STREAM>(grad, g, s);
+        default: return mix_sized<IN, OUT, 8, STREAM>(grad, g, s);
     }
+}
+
+template <class IN, class OUT>
+hipError_t mix_by_size(bool grad, const MixRowsArgs& g, hipStream_t s) {
+    return streamed((grad ? g.R_tgt : g.R_src) * g.F * (int64_t)sizeof(IN)) ? mix_by_slots<IN, OUT, true>(grad, g, s)
+                                                                           : mix_by_slots<IN, OUT, false>(grad, g, s);
 }
 
 }  // namespace
@@ -400,8 +390,8 @@ hipError_t launch_rows(bool to_rows, bool bf16, bool out_bf16, const RowsArgs& g
 }
 
 hipError_t launch_mix_rows(bool grad, bool bf16, bool out_bf16, const MixRowsArgs& g, hipStream_t s) {
-    if (bf16) return out_bf16 ? mix_by_slots<uint16_t, uint16_t>(grad, g, s) : mix_by_slots<uint16_t, float>(grad, g, s);
-    return out_bf16 ? mix_by_slots<float, uint16_t>(grad, g, s) : mix_by_slots<float, float>(grad, g, s);
+    if (bf16) return out_bf16 ? mix_by_size<uint16_t, uint16_t>(grad, g, s) : mix_by_size<uint16_t, float>(grad, g, s);
+    return out_bf16 ? mix_by_size<float, uint16_t>(grad, g, s) : mix_by_size<float, float>(grad, g, s);
 }
 
 }  // namespace pcm

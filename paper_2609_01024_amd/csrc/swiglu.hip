@@ -1,21 +1,24 @@
 // SwiGLU between the experts' two products, u = SiLU(gate) * up, and its gradient. A row of gate_up holds its gate
-// values before its up values. Bound by memory: 8 columns a thread, everything read and written once.
-#include "eight.h"
+// values before its up values. Bound by memory: 16 bytes a thread and operand, everything read and written once.
+#include "columns.h"
 
 namespace pcm {
 namespace {
 
-template <class IN, class OUT>
+template <class IN, class OUT, bool STREAM>
 __global__ __launch_bounds__(256) void swiglu_kernel(const IN* __restrict__ gate_up, const int32_t* __restrict__ count, int64_t R,
                                                      int F, OUT* __restrict__ u) {
-    const int64_t rows = count ? min(R, (int64_t)max(*count, 0)) : R, per = F / 8, total = rows * per;
+    constexpr int C = kCols<IN, OUT>;
+    const int64_t rows = count ? min(R, (int64_t)max(*count, 0)) : R, per = F / C, total = rows * per;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / per, c = (i - r * per) * 8;
-        const Eight gate = load8(gate_up + r * 2 * F + c), up = load8(gate_up + r * 2 * F + F + c);
-        Eight v;
+        const int64_t r = i / per, c = (i - r * per) * C;
+        Raw<IN, C> gate, up;
+        read<STREAM>(gate, gate_up + r * 2 * F + c);
+        read<STREAM>(up, gate_up + r * 2 * F + F + c);
+        Cols<C> v;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.v[j] = gated(IN(), gate.v[j], up.v[j]);
-        store8(u + r * F + c, v);
+        for (int j = 0; j < C; ++j) v.v[j] = gated(IN(), gate.at(j), up.at(j));
+        store_cols<C>(u + r * F + c, v);
     }
 }
 
@@ -32,32 +35,40 @@ __device__ __forceinline__ void gated_grad(float g, float up, float du, float& d
     dup = du * sig * g * more;
 }
 
-template <class IN, class OUT>
+template <class IN, class OUT, bool STREAM>
 __global__ __launch_bounds__(256) void swiglu_grad_kernel(const IN* __restrict__ gate_up, const IN* __restrict__ du,
                                                           const int32_t* __restrict__ count, int64_t R, int F,
                                                           OUT* __restrict__ dgate_up) {
-    const int64_t rows = count ? min(R, (int64_t)max(*count, 0)) : R, per = F / 8, total = rows * per;
+    constexpr int C = kCols<IN, OUT>;
+    const int64_t rows = count ? min(R, (int64_t)max(*count, 0)) : R, per = F / C, total = rows * per;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / per, c = (i - r * per) * 8;
-        const Eight gate = load8(gate_up + r * 2 * F + c), up = load8(gate_up + r * 2 * F + F + c), d = load8(du + r * F + c);
-        Eight dg, dup;
+        const int64_t r = i / per, c = (i - r * per) * C;
+        Raw<IN, C> gate, up, d;
+        read<STREAM>(gate, gate_up + r * 2 * F + c);
+        read<STREAM>(up, gate_up + r * 2 * F + F + c);
+        read<STREAM>(d, du + r * F + c);
+        Cols<C> dg, dup;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) gated_grad(gate.v[j], up.v[j], d.v[j], dg.v[j], dup.v[j]);
-        store8(dgate_up + r * 2 * F + c, dg);
-        store8(dgate_up + r * 2 * F + F + c, dup);
+        for (int j = 0; j < C; ++j) gated_grad(gate.at(j), up.at(j), d.at(j), dg.v[j], dup.v[j]);
+        store_cols<C>(dgate_up + r * 2 * F + c, dg);
+        store_cols<C>(dgate_up + r * 2 * F + F + c, dup);
     }
 }
 
-dim3 grid_of(int64_t R, int F) {
-    const int64_t blocks = ceil_div(R * (F / 8), 256);
-    return dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)));
+template <class IN, class OUT, bool STREAM>
+hipError_t swiglu_sized(const IN* gate_up, const IN* du, const int32_t* count, int64_t R, int F, OUT* out, hipStream_t s) {
+    const int64_t blocks = ceil_div(R * (F / kCols<IN, OUT>), 256);
+    const dim3 grid((unsigned)(blocks < (1 << 22) ? blocks : (1 << 22)));
+    if (du) swiglu_grad_kernel<IN, OUT, STREAM><<<grid, 256, 0, s>>>(gate_up, du, count, R, F, out);
+    else swiglu_kernel<IN, OUT, STREAM><<<grid, 256, 0, s>>>(gate_up, count, R, F, out);
+    return hipGetLastError();
 }
 
 template <class IN, class OUT>
 hipError_t swiglu_typed(const void* gate_up, const void* du, const int32_t* count, int64_t R, int F, void* out, hipStream_t s) {
-    if (du) swiglu_grad_kernel<<<grid_of(R, F), 256, 0, s>>>((const IN*)gate_up, (const IN*)du, count, R, F, (OUT*)out);
-    else swiglu_kernel<<<grid_of(R, F), 256, 0, s>>>((const IN*)gate_up, count, R, F, (OUT*)out);
-    return hipGetLastError();
+    return streamed(2 * R * F * (int64_t)sizeof(IN))
+               ? swiglu_sized<IN, OUT, true>((const IN*)gate_up, (const IN*)du, count, R, F, (OUT*)out, s)
+               : swiglu_sized<IN, OUT, false>((const IN*)gate_up, (const IN*)du, count, R, F, (OUT*)out, s);
 }
 
 }  // namespace

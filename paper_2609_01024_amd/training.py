@@ -270,7 +270,7 @@ def _tensors(tensors: Sequence[torch.Tensor], what: str):
     costs 75 ns: taken by maps, packed by slices.)"""
     T = torch.Tensor
     devices = set(map(T.get_device, tensors))
-    if devices and (devices != {torch.cuda.current_device()} or not all(map(T.is_contiguous, tensors))):
+    if devices and (min(devices) < 0 or devices != {torch.cuda.current_device()} or not all(map(T.is_contiguous, tensors))):
         raise ValueError(f"{what} must be contiguous tensors on the current device")
     try:
         codes = [_CODES[t.dtype] for t in tensors]

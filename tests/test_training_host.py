@@ -64,7 +64,7 @@ ON_GROUPS = [name for name in ON_TOKENS if "mix" not in name]
 def test_sizes_and_types(L, name):
     call, args = getattr(L, name), CALLS[name]
     for bad, want in ((dict(H=0), ARG), (dict(R=-1), ARG), (dict(H=72), UNSUP), (dict(R=1 << 30), UNSUP),
-                      (dict(H=(1 << 31) - 112), UNSUP), (dict(dt=F16DOWN), ARG), (dict(dt=-1), ARG), (dict(out=F16DOWN), ARG),
+                      (dict(H=(1 << 31) - 112), UNSUP), (dict(H=(1 << 28) + 16), UNSUP), (dict(H=1 << 28, out=-1), ARG), (dict(dt=F16DOWN), ARG), (dict(dt=-1), ARG), (dict(out=F16DOWN), ARG),
                       (dict(out=7), ARG)):
         assert call(*args(**bad)) == want, (name, bad)
     if name in ON_TOKENS:
