@@ -166,12 +166,17 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(RowsArgs g) {
 }
 
 constexpr int64_t kMostBlocks = 1 << 22;
+// Threads for a token's columns in `parts` workgroups, whole waves, the parts alike.
+int threads_of(int64_t chunks, int parts) {
+    const int64_t share = ceil_div(chunks, parts);
+    return (int)(share < kThreads ? align_up(share, 64) : kThreads);
+}
 
 template <class IN, class OUT, int KK, bool TO_ROWS, bool STREAM>
 hipError_t rows_by_dot(RowsArgs g, hipStream_t s) {
     const int64_t chunks = g.H / kCols<IN, OUT>;
-    const int threads = (int)(chunks >= kThreads ? kThreads : align_up(chunks, 64));
-    g.parts = g.dweights ? 1 : (int)ceil_div(chunks, threads);
+    g.parts = g.dweights ? 1 : (int)ceil_div(chunks, kThreads);
+    const int threads = threads_of(chunks, g.parts);
     const int64_t items = g.T * g.parts;
     const unsigned blocks = (unsigned)(items < kMostBlocks ? items : kMostBlocks);
     if (g.dweights) rows_kernel<IN, OUT, KK, TO_ROWS, true, STREAM><<<dim3(blocks), threads, 0, s>>>(g);
@@ -271,17 +276,20 @@ __global__ __launch_bounds__(kThreads) void mix_rows_kernel(MixRowsArgs g) {
     }
 }
 
-// The waves of a workgroup are shared by its tokens, `per` to each; all lanes of a wave stay active (past the last column
-// on the last ones again, as zeros), so that the sums cross the whole wave.
-template <class IN, class OUT, int K, int C, bool STREAM>
+// A wave takes A of a token's K sources, all targets and every per-th step of 64 C columns: A * K sums for dbeta in registers
+// next to the rows. All lanes of a wave stay active (past the last column on the last ones again, as zeros), so that the sums
+// cross the whole wave. Eight sources in one wave left two waves on a SIMD, waiting (8192 tokens, F 1024: 89 us; 2 x 4 SWEPT).
+template <class IN, class OUT, int K, int A, int C, bool STREAM>
 __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs g, int per) {
-    constexpr int N = pow2_above(K * K);
+    constexpr int N = pow2_above(A * K), kShares = (K + A - 1) / A;
     __shared__ float part[kGradThreads / 64][N];
     const IN* __restrict__ u = (const IN*)g.u;
     const IN* __restrict__ dz = (const IN*)g.dz;
     OUT* __restrict__ du = (OUT*)g.out;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int waves = blockDim.x / 64, tokens = waves / per, mine = wave / per, sub = wave - mine * per;
+    // waves: tokens, shares of their sources, shares of the columns
+    const int group = wave / per, sub = wave - group * per, mine = group / kShares, a0 = (group - mine * kShares) * A;
+    const int tokens = kGradThreads / 64 / per / kShares;
     for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < g.T; t0 += (int64_t)gridDim.x * tokens) {
         const int64_t t = t0 + mine;
         float dot[N];
@@ -289,53 +297,62 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
         for (int i = 0; i < N; ++i) dot[i] = 0.0f;
         if (t < g.T) {
             const Paths<K> p = paths_of<K>(g, t);
+            const uint64_t bits = p.bits >> (a0 * K);
+            const uint32_t srcs = p.srcs >> a0;
+            const Scalar<float> beta = p.beta + a0 * K;
+            int src[A];
+#pragma unroll
+            for (int a = 0; a < A; ++a) {
+                src[a] = p.src[0];
+#pragma unroll
+                for (int q = 1; q < K; ++q) src[a] = a0 + a == q ? p.src[q] : src[a];
+            }
             for (int c0 = sub * 64 * C; c0 < g.F; c0 += per * 64 * C) {
                 const int at = c0 + lane * C, c = min(at, g.F - C);
-                Raw<IN, C> v[K], d[K];
+                Raw<IN, C> v[A], d[K];
                 if (p.bits) {
 #pragma unroll
-                    for (int a = 0; a < K; ++a) {
-                        read<STREAM>(v[a], column(u, (int64_t)p.src[a] * g.F, c));
-                        read<STREAM>(d[a], column(dz, (int64_t)p.tgt[a] * g.F, c));
-                    }
+                    for (int a = 0; a < A; ++a) read<STREAM>(v[a], column(u, (int64_t)src[a] * g.F, c));
+#pragma unroll
+                    for (int b = 0; b < K; ++b) read<STREAM>(d[b], column(dz, (int64_t)p.tgt[b] * g.F, c));
                 }
                 if (c0 + 64 * C > g.F) {
 #pragma unroll
-                    for (int a = 0; a < K; ++a) {
-                        v[a].zero_unless(at < g.F);
-                        d[a].zero_unless(at < g.F);
-                    }
+                    for (int a = 0; a < A; ++a) v[a].zero_unless(at < g.F);
+#pragma unroll
+                    for (int b = 0; b < K; ++b) d[b].zero_unless(at < g.F);
                 }
 #pragma unroll
-                for (int a = 0; a < K; ++a) {
+                for (int a = 0; a < A; ++a) {
                     Cols<C> s{};
 #pragma unroll
                     for (int b = 0; b < K; ++b)
-                        if ((p.bits >> (a * K + b)) & 1) {
-                            const float w = p.beta[a * K + b];
+                        if ((bits >> (a * K + b)) & 1) {
+                            const float w = beta[a * K + b];
 #pragma unroll
                             for (int i = 0; i < C; ++i) {
                                 s.v[i] = fmaf(w, d[b].at(i), s.v[i]);
                                 dot[a * K + b] = fmaf(v[a].at(i), d[b].at(i), dot[a * K + b]);
                             }
                         }
-                    if (du && ((p.srcs >> a) & 1) && at < g.F) store_cols<C>(column(du, (int64_t)p.src[a] * g.F, at), s);
+                    if (du && ((srcs >> a) & 1) && at < g.F) store_cols<C>(column(du, (int64_t)src[a] * g.F, at), s);
                 }
             }
         }
         const float sum = wave_sums<N>(dot);
         constexpr int kLanes = 64 / N;
-        const int i = lane / kLanes;
+        const int i = lane / kLanes, left = min(A, K - a0) * K;   // elements of dbeta that this wave has
+        float* const out = g.dbeta + t * (K * K) + a0 * K;
         if (per == 1) {
-            if (t < g.T && lane % kLanes == 0 && i < K * K) g.dbeta[t * K * K + i] = sum;
+            if (t < g.T && lane % kLanes == 0 && i < left) out[i] = sum;
             continue;
         }
         if (lane % kLanes == 0) part[wave][i] = sum;
         __syncthreads();
-        if (sub == 0 && t < g.T && lane < K * K) {
+        if (sub == 0 && t < g.T && lane < left) {
             float s = 0.0f;
             for (int q = 0; q < per; ++q) s += part[wave + q][lane];
-            g.dbeta[t * K * K + lane] = s;
+            out[lane] = s;
         }
         __syncthreads();
     }
@@ -344,18 +361,17 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
 template <class IN, class OUT, int K, bool STREAM>
 hipError_t mix_sized(bool grad, MixRowsArgs g, hipStream_t s) {
     if (grad && g.dbeta) {
-        // Waves for a token: steps of 64 C columns, up to four to a wave.
-        constexpr int C = K > 4 ? 4 : kCols<IN, OUT>;
+        constexpr int A = K > 4 ? (K + 1) / 2 : K, C = K > 4 ? 4 : kCols<IN, OUT>, kWaves = kGradThreads / 64 / (K > 4 ? 2 : 1);
         const int64_t steps = ceil_div(g.F, 64 * C);
-        const int per = steps <= 4 ? 1 : steps <= 8 ? 2 : 4, tokens = kGradThreads / 64 / per;
-        const int64_t blocks = ceil_div(g.T, tokens);
-        mix_rows_grad_kernel<IN, OUT, K, C, STREAM>
+        const int per = steps <= 4 ? 1 : steps <= 8 || kWaves == 2 ? 2 : 4;
+        const int64_t blocks = ceil_div(g.T, kWaves / per);
+        mix_rows_grad_kernel<IN, OUT, K, A, C, STREAM>
             <<<dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), kGradThreads, 0, s>>>(g, per);
         return hipGetLastError();
     }
     const int64_t chunks = g.F / kCols<IN, OUT>;
-    const int threads = (int)(chunks >= kThreads ? kThreads : align_up(chunks, 64));
-    g.parts = (int)ceil_div(chunks, threads);
+    g.parts = (int)ceil_div(chunks, kThreads);
+    const int threads = threads_of(chunks, g.parts);
     const int64_t items = g.T * g.parts;
     const dim3 grid((unsigned)(items < kMostBlocks ? items : kMostBlocks));
     if (grad) mix_rows_kernel<IN, OUT, K, true, STREAM><<<grid, threads, 0, s>>>(g);
