@@ -25,7 +25,8 @@ __device__ __forceinline__ Eight load8(const float* p) {
 }
 
 // C neighbouring columns as they are read. They stay so until they are used, so that all of a thread's loads are on their
-// way before the first wait.
+// way before the first wait. arrived(): waits for them here. Where they are used under branches, with stores between, the
+// compiler waits again at every use, and a wait for a load is one for the stores before it too.
 template <class T, int C>
 struct Raw;
 template <int C>
@@ -39,6 +40,7 @@ struct Raw<uint16_t, C> {
 #pragma unroll
         for (int i = 0; i < C / 2; ++i) w[i] = keep ? w[i] : 0u;
     }
+    __device__ __forceinline__ void arrived() { asm volatile("" : "+v"(w)); }
 };
 template <int C>
 struct Raw<float, C> {
@@ -56,16 +58,22 @@ struct Raw<float, C> {
 #pragma unroll
         for (int i = 0; i < C; ++i) w[i / 4][i % 4] = keep ? w[i / 4][i % 4] : 0.0f;
     }
+    __device__ __forceinline__ void arrived() {
+#pragma unroll
+        for (int i = 0; i < C / 4; ++i) asm volatile("" : "+v"(w[i]));
+    }
 };
 template <bool STREAM, class T, int C>
 __device__ __forceinline__ void read(Raw<T, C>& r, const T* p) {
     if constexpr (STREAM) r.stream(p);
     else r.load(p);
 }
-// Operands over half of the 256 MB of the last cache level are loaded non-temporally (`stream`): they are not in it, and
-// what is stays there (SwiGLU gradient of 554 MB read 160 us -> 145). Smaller ones may be there from the kernel
-// that wrote them (dispatch of 34 MB to 268: 51 us, 57 so).
-inline bool streamed(int64_t bytes) { return bytes > (int64_t)128 << 20; }
+// From 96 MB read on operands are loaded non-temporally: they are then hardly in the 256 MB of the last cache level, which the
+// kernel that wrote them and this one's results share. us, non-temporally / plainly, tensors used in turn: SwiGLU 64 MB read 17.4 /
+// 15.6, 128 MB 32.6 / 34.3, its gradient 48 MB 15.7 / 14.5, 96 MB 27.8 / 29.4; combine 64 MB 15.1 / 14.2, 128 MB 28.5 / 31.1, its
+// gradient 80 MB 26.8 / 24.1, 160 MB 48.8 / 56.0; mix 64 MB 26.0 / 22.4, 128 MB 48.2 / 52.0, its gradient 64 MB 19.8 / 18.2, 128 MB
+// 39.8 / 42.3.
+inline bool streamed(int64_t bytes) { return bytes >= (int64_t)96 << 20; }
 // Columns a thread takes: 16 bytes of float32, where there is any, or of bf16, so that a wave's access is one piece.
 template <class IN, class OUT>
 constexpr int kCols = sizeof(IN) == 2 && sizeof(OUT) == 2 ? 8 : 4;

@@ -194,7 +194,7 @@ hipError_t rows_by_slots(const RowsArgs& g, hipStream_t s) {
 
 template <class IN, class OUT, bool TO_ROWS>
 hipError_t rows_by_size(const RowsArgs& g, hipStream_t s) {
-    return streamed(g.R * g.H * (int64_t)sizeof(IN)) ? rows_by_slots<IN, OUT, TO_ROWS, true>(g, s)
+    return streamed((g.R + (g.tokens ? g.T : 0)) * g.H * (int64_t)sizeof(IN)) ? rows_by_slots<IN, OUT, TO_ROWS, true>(g, s)
                                                      : rows_by_slots<IN, OUT, TO_ROWS, false>(g, s);
 }
 
@@ -251,11 +251,16 @@ __global__ __launch_bounds__(kThreads) void mix_rows_kernel(MixRowsArgs g) {
         const int64_t t = g.parts == 1 ? item : item / g.parts;
         const int part0 = (int)(item - t * g.parts);
         const Paths<K> p = paths_of<K>(g, t);
+        float beta[K * K];
+#pragma unroll
+        for (int i = 0; i < K * K; ++i) beta[i] = p.beta[i];
         for (int c = (part0 * blockDim.x + threadIdx.x) * C; c < g.F; c += g.parts * blockDim.x * C) {
             Raw<IN, C> v[K];
             if (p.bits) {
 #pragma unroll
                 for (int a = 0; a < K; ++a) read<STREAM>(v[a], column(in, (int64_t)(BACK ? p.tgt[a] : p.src[a]) * g.F, c));
+#pragma unroll
+                for (int a = 0; a < K; ++a) v[a].arrived();
             }
 #pragma unroll
             for (int b = 0; b < K; ++b) {
@@ -265,7 +270,7 @@ __global__ __launch_bounds__(kThreads) void mix_rows_kernel(MixRowsArgs g) {
                 for (int a = 0; a < K; ++a) {
                     const int i = BACK ? b * K + a : a * K + b;
                     if ((p.bits >> i) & 1) {
-                        const float w = p.beta[i];
+                        const float w = beta[i];
 #pragma unroll
                         for (int q = 0; q < C; ++q) s.v[q] = fmaf(w, v[a].at(q), s.v[q]);
                     }
@@ -282,13 +287,14 @@ __global__ __launch_bounds__(kThreads) void mix_rows_kernel(MixRowsArgs g) {
 template <class IN, class OUT, int K, int A, int C, bool STREAM>
 __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs g, int per) {
     constexpr int N = pow2_above(A * K), kShares = (K + A - 1) / A;
+    constexpr bool kTwice = kShares * A > K;
     __shared__ float part[kGradThreads / 64][N];
     const IN* __restrict__ u = (const IN*)g.u;
     const IN* __restrict__ dz = (const IN*)g.dz;
     OUT* __restrict__ du = (OUT*)g.out;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // waves: tokens, shares of their sources, shares of the columns
-    const int group = wave / per, sub = wave - group * per, mine = group / kShares, a0 = (group - mine * kShares) * A;
+    const int group = wave / per, sub = wave - group * per, mine = group / kShares, share = group - mine * kShares, a0 = share ? K - A : 0;
     const int tokens = kGradThreads / 64 / per / kShares;
     for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < g.T; t0 += (int64_t)gridDim.x * tokens) {
         const int64_t t = t0 + mine;
@@ -297,9 +303,12 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
         for (int i = 0; i < N; ++i) dot[i] = 0.0f;
         if (t < g.T) {
             const Paths<K> p = paths_of<K>(g, t);
-            const uint64_t bits = p.bits >> (a0 * K);
-            const uint32_t srcs = p.srcs >> a0;
-            const Scalar<float> beta = p.beta + a0 * K;
+            // (of an odd number the source in the middle is the first share's)
+            const uint64_t bits = share && kTwice ? p.bits >> (a0 * K) & ~(((uint64_t)1 << K) - 1) : p.bits >> (a0 * K);
+            const uint32_t srcs = share && kTwice ? p.srcs >> a0 & ~1u : p.srcs >> a0;
+            float beta[A * K];
+#pragma unroll
+            for (int i = 0; i < A * K; ++i) beta[i] = p.beta[a0 * K + i];
             int src[A];
 #pragma unroll
             for (int a = 0; a < A; ++a) {
@@ -314,7 +323,11 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
 #pragma unroll
                     for (int a = 0; a < A; ++a) read<STREAM>(v[a], column(u, (int64_t)src[a] * g.F, c));
 #pragma unroll
-                    for (int b = 0; b < K; ++b) read<STREAM>(d[b], column(dz, (int64_t)p.tgt[b] * g.F, c));
+                    for (int b = 0; b < K; ++b) read<STREAM && kShares == 1>(d[b], column(dz, (int64_t)p.tgt[b] * g.F, c));
+#pragma unroll
+                    for (int a = 0; a < A; ++a) v[a].arrived();
+#pragma unroll
+                    for (int b = 0; b < K; ++b) d[b].arrived();
                 }
                 if (c0 + 64 * C > g.F) {
 #pragma unroll
@@ -341,15 +354,15 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
         }
         const float sum = wave_sums<N>(dot);
         constexpr int kLanes = 64 / N;
-        const int i = lane / kLanes, left = min(A, K - a0) * K;   // elements of dbeta that this wave has
+        const int i = lane / kLanes, skip = share && kTwice ? K : 0;   // elements of dbeta [skip, A K) are this wave's
         float* const out = g.dbeta + t * (K * K) + a0 * K;
         if (per == 1) {
-            if (t < g.T && lane % kLanes == 0 && i < left) out[i] = sum;
+            if (t < g.T && lane % kLanes == 0 && i >= skip && i < A * K) out[i] = sum;
             continue;
         }
         if (lane % kLanes == 0) part[wave][i] = sum;
         __syncthreads();
-        if (sub == 0 && t < g.T && lane < left) {
+        if (sub == 0 && t < g.T && lane >= skip && lane < A * K) {
             float s = 0.0f;
             for (int q = 0; q < per; ++q) s += part[wave + q][lane];
             out[lane] = s;
@@ -395,7 +408,7 @@ hipError_t mix_by_slots(bool grad, const MixRowsArgs& g, hipStream_t s) {
 
 template <class IN, class OUT>
 hipError_t mix_by_size(bool grad, const MixRowsArgs& g, hipStream_t s) {
-    return streamed((grad ? g.R_tgt : g.R_src) * g.F * (int64_t)sizeof(IN)) ? mix_by_slots<IN, OUT, true>(grad, g, s)
+    return streamed(((g.u ? g.R_src : 0) + (grad ? g.R_tgt : 0)) * g.F * (int64_t)sizeof(IN)) ? mix_by_slots<IN, OUT, true>(grad, g, s)
                                                                            : mix_by_slots<IN, OUT, false>(grad, g, s);
 }
 

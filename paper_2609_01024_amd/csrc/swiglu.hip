@@ -66,7 +66,7 @@ hipError_t swiglu_sized(const IN* gate_up, const IN* du, const int32_t* count, i
 
 template <class IN, class OUT>
 hipError_t swiglu_typed(const void* gate_up, const void* du, const int32_t* count, int64_t R, int F, void* out, hipStream_t s) {
-    return streamed(2 * R * F * (int64_t)sizeof(IN))
+    return streamed((du ? 3 : 2) * R * F * (int64_t)sizeof(IN))
                ? swiglu_sized<IN, OUT, true>((const IN*)gate_up, (const IN*)du, count, R, F, (OUT*)out, s)
                : swiglu_sized<IN, OUT, false>((const IN*)gate_up, (const IN*)du, count, R, F, (OUT*)out, s);
 }
