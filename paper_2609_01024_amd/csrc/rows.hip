@@ -12,7 +12,12 @@
 namespace pcm {
 namespace {
 
-constexpr int kThreads = 256, kGradThreads = 256;
+constexpr int kThreads = 256, kGradThreads = 1024;
+// Threads at most for a token where its products are summed over the workgroup: one pass over the columns where it goes (dispatch
+// gradient, float32, 8192 x 4 of 2048: 512 threads 63.0 us, 256 66.8; 2048 x 8 of 7168: 51.8 / 51.6, 1024 62.5); towards the
+// rows two (combine gradient, 2048 x 8 of 7168: 256 threads 96.4 us, 512 100.5; 4096 x 2 of 4096: 30.4 / 29.8).
+template <bool TO_ROWS>
+constexpr int kDotThreads = TO_ROWS ? 256 : 512;
 
 constexpr int pow2_above(int v) { return v <= 1 ? 1 : 2 * pow2_above((v + 1) / 2); }
 
@@ -81,9 +86,9 @@ __device__ __forceinline__ T* column(T* __restrict__ p, int64_t row, uint32_t c)
 // TO_ROWS: dispatch and the combine's gradient, from `tokens` to the rows of out; otherwise combine and the dispatch's
 // gradient, from `rows` to the tokens of out. DOT: dweights too, from both.
 template <class IN, class OUT, int KK, bool TO_ROWS, bool DOT, bool STREAM>
-__global__ __launch_bounds__(kThreads) void rows_kernel(RowsArgs g) {
+__global__ __launch_bounds__(DOT ? kDotThreads<TO_ROWS> : kThreads) void rows_kernel(RowsArgs g) {
     constexpr int C = kCols<IN, OUT>;
-    __shared__ float part[kThreads / 64][KK];
+    __shared__ float part[kDotThreads<TO_ROWS> / 64][KK];
     const IN* __restrict__ tokens = (const IN*)g.tokens;
     const IN* __restrict__ rows = (const IN*)g.rows;
     OUT* __restrict__ out = (OUT*)g.out;
@@ -165,22 +170,27 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(RowsArgs g) {
     }
 }
 
-constexpr int64_t kMostBlocks = 1 << 22;
+constexpr int64_t kMostBlocks = 1 << 21;   // of up to 1024 threads, whose number is held in 32 bits
 // Threads for a token's columns in `parts` workgroups, whole waves, the parts alike.
-int threads_of(int64_t chunks, int parts) {
+int threads_of(int64_t chunks, int parts, int most) {
     const int64_t share = ceil_div(chunks, parts);
-    return (int)(share < kThreads ? align_up(share, 64) : kThreads);
+    return (int)(share < most ? align_up(share, 64) : most);
 }
 
 template <class IN, class OUT, int KK, bool TO_ROWS, bool STREAM>
 hipError_t rows_by_dot(RowsArgs g, hipStream_t s) {
     const int64_t chunks = g.H / kCols<IN, OUT>;
-    g.parts = g.dweights ? 1 : (int)ceil_div(chunks, kThreads);
-    const int threads = threads_of(chunks, g.parts);
+    if (g.dweights) {
+        g.parts = 1;
+        const unsigned blocks = (unsigned)(g.T < kMostBlocks ? g.T : kMostBlocks);
+        const int threads = threads_of(chunks, (int)ceil_div(chunks, kDotThreads<TO_ROWS>), kDotThreads<TO_ROWS>);
+        rows_kernel<IN, OUT, KK, TO_ROWS, true, STREAM><<<dim3(blocks), threads, 0, s>>>(g);
+        return hipGetLastError();
+    }
+    g.parts = (int)ceil_div(chunks, kThreads);
     const int64_t items = g.T * g.parts;
     const unsigned blocks = (unsigned)(items < kMostBlocks ? items : kMostBlocks);
-    if (g.dweights) rows_kernel<IN, OUT, KK, TO_ROWS, true, STREAM><<<dim3(blocks), threads, 0, s>>>(g);
-    else rows_kernel<IN, OUT, KK, TO_ROWS, false, STREAM><<<dim3(blocks), threads, 0, s>>>(g);
+    rows_kernel<IN, OUT, KK, TO_ROWS, false, STREAM><<<dim3(blocks), threads_of(chunks, g.parts, kThreads), 0, s>>>(g);
     return hipGetLastError();
 }
 
@@ -295,7 +305,7 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // waves: tokens, shares of their sources, shares of the columns
     const int group = wave / per, sub = wave - group * per, mine = group / kShares, share = group - mine * kShares, a0 = share ? K - A : 0;
-    const int tokens = kGradThreads / 64 / per / kShares;
+    const int tokens = blockDim.x / 64 / per / kShares;
     for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < g.T; t0 += (int64_t)gridDim.x * tokens) {
         const int64_t t = t0 + mine;
         float dot[N];
@@ -374,17 +384,20 @@ __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs
 template <class IN, class OUT, int K, bool STREAM>
 hipError_t mix_sized(bool grad, MixRowsArgs g, hipStream_t s) {
     if (grad && g.dbeta) {
-        constexpr int A = K > 4 ? (K + 1) / 2 : K, C = K > 4 ? 4 : kCols<IN, OUT>, kWaves = kGradThreads / 64 / (K > 4 ? 2 : 1);
-        const int64_t steps = ceil_div(g.F, 64 * C);
-        const int per = steps <= 4 ? 1 : steps <= 8 || kWaves == 2 ? 2 : 4;
-        const int64_t blocks = ceil_div(g.T, kWaves / per);
+        // A step of 64 C columns a wave (few experts, 7 steps / 1: 131 / 122 us; top-4, F 1408, 3 steps / 1: 107 / 104); where a
+        // wave's sums are many, four (top-8, F 1024, 4 steps / 2 / 1: 82 / 85 / 113). At least four waves a workgroup.
+        constexpr int A = K > 4 ? (K + 1) / 2 : K, C = K > 4 ? 4 : kCols<IN, OUT>, kShares = K > 4 ? 2 : 1, kSteps = K > 4 ? 4 : 1;
+        constexpr int kMost = kGradThreads / 64 / kShares;
+        const int64_t wanted = ceil_div(g.F, 64 * C * kSteps);
+        const int per = (int)(wanted < kMost ? wanted : kMost), tokens = per * kShares < 4 ? 4 / (per * kShares) : 1;
+        const int64_t blocks = ceil_div(g.T, tokens);
         mix_rows_grad_kernel<IN, OUT, K, A, C, STREAM>
-            <<<dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), kGradThreads, 0, s>>>(g, per);
+            <<<dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), per * kShares * tokens * 64, 0, s>>>(g, per);
         return hipGetLastError();
     }
     const int64_t chunks = g.F / kCols<IN, OUT>;
     g.parts = (int)ceil_div(chunks, kThreads);
-    const int threads = threads_of(chunks, g.parts);
+    const int threads = threads_of(chunks, g.parts, kThreads);
     const int64_t items = g.T * g.parts;
     const dim3 grid((unsigned)(items < kMostBlocks ? items : kMostBlocks));
     if (grad) mix_rows_kernel<IN, OUT, K, true, STREAM><<<grid, threads, 0, s>>>(g);
