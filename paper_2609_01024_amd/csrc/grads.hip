@@ -88,10 +88,16 @@ __global__ __launch_bounds__(kTokens * kMaxK) void route_grad_kernel(RouteGradAr
 }
 
 // ---------------------------------------------------------------- all gradients
-// A launch takes up to GradTable::kMost tensors, cut into chunks of 16 KB (of what is read) that begin at multiples of 16
-// bytes, wherever the tensor does: four 16-byte vectors a thread. The vectors at a tensor's ends that hold other bytes
-// too go by elements. Squares and their sums are 64 bits: no gradient that float32 holds overflows or vanishes in them.
-constexpr int kChunk = 16384, kNormThreads = 256, kVectors = kChunk / 16 / kNormThreads;
+// A launch takes up to GradTable::kMost tensors, cut into chunks (of what is read) that begin at multiples of 16 bytes, wherever
+// the tensor does. The vectors of 16 bytes at a tensor's ends that hold other bytes too go by elements. Squares and their
+// sums are 64 bits: no gradient that float32 holds overflows or vanishes in them; nor do they cost time (1.4 G elements of bf16
+// 445 us with sums of 8 in 32 bits too).
+// Chunks of 4 vectors a thread for the norm, whose workgroups, six on a compute unit, all of them at once, take every so-manyeth
+// chunk (1.4 G bf16, 100 M float32: 408 and 68 us, 6.9 and 5.9 TB/s; 2048 workgroups 445 and 86; 2 vectors and eight on a compute
+// unit 426 and 65; 1 520 and 78), of 2 for the clipping, a chunk a workgroup: what writes runs at 6.5 TB/s read and
+// written that way and at 5 with workgroups that loop (100 M float32, both passes: 2 vectors 193 us, 4 201, 1 208).
+constexpr int kNormThreads = 256, kNormVectors = 4, kClipVectors = 2;
+constexpr int chunk_bytes(int vectors) { return vectors * 16 * kNormThreads; }
 constexpr int kFewParts = 256;   // sums that every workgroup of the clipping adds itself, instead of a launch that does
 
 __device__ __forceinline__ double block_sum(double v, double* part) {
@@ -148,19 +154,19 @@ __device__ __forceinline__ void put(float* p, int64_t i, float v) { p[i] = v; }
 
 // Chunk j of a tensor of `count` elements at p: whole(first element, vector) for each vector inside, part(element) for
 // each element of the others. All vectors are loaded first.
-template <class T, class WHOLE, class PART>
+template <int V, class T, class WHOLE, class PART>
 __device__ __forceinline__ void each_vector(const T* p, int64_t count, int64_t j, WHOLE whole, PART part) {
     constexpr int N = Vec<T>::N;
     const int64_t before = ((uintptr_t)p & 15) / sizeof(T);     // elements of the first vector that lie before p
-    const int64_t e0 = j * (kChunk / (int64_t)sizeof(T)) - before + threadIdx.x * N;
-    uintx4 w[kVectors];
+    const int64_t e0 = j * (chunk_bytes(V) / (int64_t)sizeof(T)) - before + threadIdx.x * N;
+    uintx4 w[V];
 #pragma unroll
-    for (int i = 0; i < kVectors; ++i) {
+    for (int i = 0; i < V; ++i) {
         const int64_t e = e0 + i * (kNormThreads * N);
         if (e >= 0 && e + N <= count) w[i] = __builtin_nontemporal_load((const uintx4*)(p + e));
     }
 #pragma unroll
-    for (int i = 0; i < kVectors; ++i) {
+    for (int i = 0; i < V; ++i) {
         const int64_t e = e0 + i * (kNormThreads * N);
         if (e >= 0 && e + N <= count) whole(e, unpacked(p, w[i]));
         else
@@ -172,7 +178,7 @@ __device__ __forceinline__ void each_vector(const T* p, int64_t count, int64_t j
 template <class T>
 __device__ __forceinline__ double chunk_squares(const T* p, int64_t count, int64_t j) {
     double s[4] = {0.0, 0.0, 0.0, 0.0};
-    each_vector(
+    each_vector<kNormVectors>(
         p, count, j,
         [&](int64_t, const Vec<T>& x) {
 #pragma unroll
@@ -217,7 +223,7 @@ __device__ __forceinline__ void chunk_scaled(const IN* p, OUT* q, int64_t count,
     constexpr int N = Vec<IN>::N, kBytes = N * (int)sizeof(OUT) < 16 ? N * (int)sizeof(OUT) : 16;
     // (an output whose elements lie otherwise than the input's to multiples of a vector)
     const bool aligned = (((uintptr_t)q - ((uintptr_t)p & 15) / sizeof(IN) * sizeof(OUT)) & (kBytes - 1)) == 0;
-    each_vector(
+    each_vector<kClipVectors>(
         p, count, j,
         [&](int64_t e, const Vec<IN>& x) {
             if (!aligned) {
@@ -225,23 +231,20 @@ __device__ __forceinline__ void chunk_scaled(const IN* p, OUT* q, int64_t count,
                 for (int i = 0; i < N; ++i) put(q, e + i, x.v[i] * f);
                 return;
             }
-            if constexpr (sizeof(OUT) == 4) {
+            Cols<N> y;
 #pragma unroll
-                for (int i = 0; i < N; i += 4)
-                    *(floatx4*)(q + e + i) = floatx4{x.v[i] * f, x.v[i + 1] * f, x.v[i + 2] * f, x.v[i + 3] * f};
-            } else {
-                typedef __bf16 out_t __attribute__((ext_vector_type(N)));
-                out_t y;
+            for (int i = 0; i < N; ++i) y.v[i] = x.v[i] * f;
+            if constexpr (N * sizeof(OUT) <= 16) {
+                store_cols<N>(q + e, y);
+            } else {   // two stores of neighbouring halves: their lines fill up in the cache (100 M bf16 147 us; not kept 164)
 #pragma unroll
-                for (int i = 0; i < N; ++i) y[i] = (__bf16)(x.v[i] * f);
-                *(out_t*)(q + e) = y;
+                for (int i = 0; i < N; i += 4) *(floatx4*)(q + e + i) = floatx4{y.v[i], y.v[i + 1], y.v[i + 2], y.v[i + 3]};
             }
         },
         [&](int64_t e) { put(q, e, element(p, e) * f); });
 }
 
-// parts: the norm is formed from them here (and written by the first workgroup); otherwise it is read. A chunk a
-// workgroup: writing goes at 6.5 TB/s read and written that way, at 5 with workgroups that loop.
+// parts: the norm is formed from them here (and written by the first workgroup); otherwise it is read.
 __global__ __launch_bounds__(kNormThreads) void clip_kernel(GradTable g, const double* parts, int count, float* norm, int write_norm,
                                                             float max_norm) {
     __shared__ double red[kNormThreads / 64];
@@ -265,7 +268,7 @@ __global__ __launch_bounds__(kNormThreads) void clip_kernel(GradTable g, const d
 }
 
 // The table of grads[0, m); false where its chunks are too many to count.
-bool table_of(const pcm_tensor* in, const pcm_tensor* out, int m, GradTable* g) {
+bool table_of(const pcm_tensor* in, const pcm_tensor* out, int m, int chunk, GradTable* g) {
     uint64_t chunks = 0;
     g->m = m;
     for (int i = 0; i < m; ++i) {
@@ -275,7 +278,7 @@ bool table_of(const pcm_tensor* in, const pcm_tensor* out, int m, GradTable* g) 
         g->count[i] = in[i].count;
         g->type[i] = (uint8_t)((in[i].dtype == PCM_BF16 ? 1 : 0) | ((out ? out[i] : in[i]).dtype == PCM_BF16 ? 2 : 0));
         g->start[i] = (uint32_t)chunks;
-        if (in[i].count) chunks += (uint64_t)ceil_div((int64_t)((uintptr_t)in[i].data & 15) + in[i].count * size, kChunk);
+        if (in[i].count) chunks += (uint64_t)ceil_div((int64_t)((uintptr_t)in[i].data & 15) + in[i].count * size, chunk);
         if (chunks >> 31) return false;
     }
     g->start[m] = (uint32_t)chunks;
@@ -302,7 +305,7 @@ hipError_t launch_grad_norm(const pcm_tensor* in, const pcm_tensor* out, int m, 
     GradTable g;
     if (parts) {
         for (int at = 0; at < m; at += kMost) {
-            if (!table_of(in + at, nullptr, m - at < kMost ? m - at : kMost, &g)) return hipErrorInvalidValue;
+            if (!table_of(in + at, nullptr, m - at < kMost ? m - at : kMost, chunk_bytes(kNormVectors), &g)) return hipErrorInvalidValue;
             const uint32_t chunks = g.start[g.m], blocks = chunks < kGradBlocks ? chunks : kGradBlocks;
             if (!blocks) continue;
             norm_kernel<<<blocks, kNormThreads, 0, s>>>(g, parts + count);
@@ -316,7 +319,8 @@ hipError_t launch_grad_norm(const pcm_tensor* in, const pcm_tensor* out, int m, 
     }
     bool first = true;
     for (int at = 0; at < m; at += kMost) {
-        if (!table_of(in + at, out ? out + at : nullptr, m - at < kMost ? m - at : kMost, &g)) return hipErrorInvalidValue;
+        if (!table_of(in + at, out ? out + at : nullptr, m - at < kMost ? m - at : kMost, chunk_bytes(kClipVectors), &g))
+            return hipErrorInvalidValue;
         const uint32_t chunks = g.start[g.m], blocks = chunks < (1u << 22) ? chunks : (1u << 22);
         if (!blocks) continue;
         clip_kernel<<<blocks, kNormThreads, 0, s>>>(g, parts, count, norm, first, max_norm);

@@ -345,7 +345,7 @@ struct GradTable {
     uint8_t type[kMost];         // bit 0: src is bf16, bit 1: dst is
     int m;
 };
-constexpr int kGradBlocks = 2048;   // workgroups of a launch
+constexpr int kGradBlocks = 1536;   // workgroups of a launch of the norm
 size_t grad_norm_ws_bytes(int64_t m);
 // parts: the norm is formed (in grad_norm_ws_bytes(m)) and written, otherwise read; clip: out (NULL: in) = in * factor.
 hipError_t launch_grad_norm(const pcm_tensor* in, const pcm_tensor* out, int m, bool clip, float max_norm, float* norm, double* parts,
