@@ -93,12 +93,14 @@ __global__ __launch_bounds__(kTokens * kMaxK) void route_grad_kernel(RouteGradAr
 // sums are 64 bits: no gradient that float32 holds overflows or vanishes in them; nor do they cost time (1.4 G elements of bf16
 // 445 us with sums of 8 in 32 bits too).
 // Chunks of 4 vectors a thread for the norm, whose workgroups, six on a compute unit, all of them at once, take every so-manyeth
-// chunk (1.4 G bf16, 100 M float32: 408 and 68 us, 6.9 and 5.9 TB/s; 2048 workgroups 445 and 86; 2 vectors and eight on a compute
+// chunk (1.4 G bf16, 100 M float32: 410 and 68 us, 6.9 and 5.9 TB/s; 2048 workgroups 445 and 86; 2 vectors and eight on a compute
 // unit 426 and 65; 1 520 and 78), of 2 for the clipping, a chunk a workgroup: what writes runs at 6.5 TB/s read and
 // written that way and at 5 with workgroups that loop (100 M float32, both passes: 2 vectors 193 us, 4 201, 1 208).
 constexpr int kNormThreads = 256, kNormVectors = 4, kClipVectors = 2;
 constexpr int chunk_bytes(int vectors) { return vectors * 16 * kNormThreads; }
-constexpr int kFewParts = 256;   // sums that every workgroup of the clipping adds itself, instead of a launch that does
+// Sums of so many workgroups are added by every workgroup of the clipping, instead of by a launch of their own (us, without /
+// with it: 8 MB 17.8 / 20.7, 16 MB 18.2 / 20.9, 24 MB 22.6 / 22.6, 48 MB, of 1536 sums, 35.4 / 33.8).
+constexpr int kFewParts = kGradBlocks - 1;
 
 __device__ __forceinline__ double block_sum(double v, double* part) {
 #pragma unroll
