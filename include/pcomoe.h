@@ -476,8 +476,9 @@ typedef struct pcm_tensor {
 } pcm_tensor;
 
 /* The norm over all gradients: norm [1] f32 (device) = sqrt(sum of squares of every element of grads[0, m)), squares and
- * sums in 64 bits, the norm rounded (over float32's largest: infinite). `grads` is host memory, read before the call returns; m <= 4096.
- * ws: pcm_workspace_bytes(PCM_OP_GRAD_NORM, m, 0, 0, 1, 1, 0) bytes. */
+ * sums in 64 bits, the norm rounded (over float32's largest: infinite). `grads` is host memory, read before the
+ * call returns; m <= 4096.
+ * ws: pcm_workspace_bytes(PCM_OP_GRAD_NORM, m, 0, 0, 1, 1, 0) bytes. Calls that overlap in time must not share it. */
 pcm_status pcm_grad_norm(const pcm_tensor* grads, int m, float* norm, void* ws, size_t ws_bytes, void* stream);
 
 /* Clipping by a norm on the device (pcm_grad_norm's, or one made of several ranks'): with norm > max_norm, out[i] =
@@ -487,7 +488,8 @@ pcm_status pcm_grad_norm(const pcm_tensor* grads, int m, float* norm, void* ws, 
 pcm_status pcm_clip_grads(const pcm_tensor* grads, const pcm_tensor* out, int m, const float* norm,
                           float max_norm, void* stream);
 
-/* Both, with the same results, in one pass of launches less: norm [1] f32 is written. Arguments as above. */
+/* Both, with the same results, in fewer launches where the gradients are small: norm [1] f32 is written. Arguments as
+ * above. */
 pcm_status pcm_clip_grad_norm(const pcm_tensor* grads, const pcm_tensor* out, int m, float max_norm,
                               float* norm, void* ws, size_t ws_bytes, void* stream);
 

@@ -213,6 +213,43 @@ def test_groups_bounds_are_held_inside():
         assert int((y != 7.0).any(1).sum()) == end - first, off
 
 
+def test_a_part_of_the_offsets():
+    """A rank's part of a table's offsets, as a view that starts at any of them."""
+    c = tokens_and_rows((50, 2, 7, 96), BF, "all", 6)
+    off = routed(50, 2, 7, 6)["off"].to(DEV)
+    for a, b in ((1, 4), (2, 3), (3, 7), (0, 7)):
+        on = (c["of"] >= int(off[a])) & (c["of"] < int(off[b]))
+        want = torch.where(on[:, :, None], c["o"].double()[c["of"].long()], 0.0)
+        y = pcm.pcm_combine_rows(gpu(c["o"]), gpu(c["of"]), None, off[a:b + 1], out_dtype=F32)
+        close(y, want.sum(1), 3 * U * want.abs().sum(1), (a, b))
+
+
+@pytest.mark.parametrize("H", [80, 4112])
+@pytest.mark.parametrize("types", ["bf16-f32", "f32-f32"])
+def test_products_alone(types, H):
+    """The C entry points without the tensor gradient: dweights and dbeta as with it."""
+    dt, out = TYPES[types]
+    T, k, n = 30, 3, 5
+    c = tokens_and_rows((T, k, n, H), dt, "all", 3)
+    m = path_case(T, k, n, H, dt, 0.4, 3)
+    code = binding.PCM_BF16 if dt == BF else binding.PCM_F32
+    x, o, of, w, bits, beta, u, dz = (gpu(v) for v in (c["x"], c["o"], c["of"], c["w"], m["bits"], m["beta"], m["u"], m["dz"]))
+    got = torch.full((T, k), 7.0, device=DEV)
+    L, P, R = pcm.lib(), torch.Tensor.data_ptr, T * k
+    assert L.pcm_dispatch_rows_grad(code, 0, P(o), P(x), P(of), P(w), None, T, k, R, H, 1, None, P(got), None) == 0
+    torch.cuda.synchronize()
+    same_bits(got, pcm.pcm_dispatch_rows_grad(o, of, x, w, out_dtype=F32)[1])
+    got.fill_(7.0)
+    assert L.pcm_combine_rows_grad(code, 0, P(x), P(o), P(of), P(w), None, T, k, R, H, 1, None, P(got), None) == 0
+    torch.cuda.synchronize()
+    same_bits(got, pcm.pcm_combine_rows_grad(x, of, o, w, out_dtype=F32)[1])
+    got = torch.full((T, k, k), 7.0, device=DEV)
+    mof = gpu(m["of"])
+    assert L.pcm_mix_rows_grad(code, 0, P(dz), P(u), P(bits), P(beta), P(mof), P(mof), T, k, R, R, H, None, P(got), None) == 0
+    torch.cuda.synchronize()
+    same_bits(got, pcm.pcm_mix_rows_grad(dz, u, bits, beta, mof, out_dtype=F32)[1])
+
+
 def test_rows_past_32_bits():
     """Rows whose first element lies past 2^31: the last ones of a buffer of 4.6 GB."""
     R, H, k = 1_100_000, 2080, 2
@@ -242,8 +279,8 @@ def test_rows_past_32_bits():
 
 
 def test_many_tokens():
-    """More tokens than a launch has workgroups."""
-    T, H = 1_200_001, 16
+    """More tokens than a launch has workgroups (2^21, of four tokens in the mix gradient)."""
+    T, H = 8_500_001, 16
     x = torch.randint(-3, 4, (T, H), generator=torch.Generator().manual_seed(1)).to(BF)
     of = torch.randperm(T, generator=torch.Generator().manual_seed(2)).int()[:, None]
     X, OF = gpu(x), gpu(of)
