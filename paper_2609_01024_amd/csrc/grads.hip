@@ -15,7 +15,7 @@ namespace {
 //   SRC_COND A_c = h_c = G_c / S_c;   PRODUCT A_c = G_c, h = 0;   GLOBAL h = sum_a p_a G_a / Z, A_c = (G_c - h S_c) / Z,
 // and by the logits dl_a = p_a (dp_a - sum_c p_c dp_c). S_a = 0 (every p of T_a, p_a among them, below float32's range):
 // what it would scale is multiplied by a zero p, so nothing is. Differences of sums that are near to each other: 64 bits.
-// Bound by its launch and by writing [T, n]: 8 threads a token, the rows of 32 tokens built in LDS.
+// Bound by its launch and by writing [T, n]: 8 threads a token, the rows of 32 tokens built in LDS (16384 x 60: 5.5 us).
 constexpr int kTokens = 32;
 
 template <class OUT>

@@ -7,6 +7,10 @@
 //   its gradient    du[src_a] = sum_b beta_ab dz[tgt_b],   dbeta_ab = <dz[tgt_b], u[src_a]>
 // All are bound by memory. A workgroup takes a token: the token's row numbers and weights are scalars there, and what
 // the rows of a token share (its own row, or the sum) is read or written once. Sums are float32, slots ascending.
+// Measured, bf16 (a copy of 2 GB moves 6.5 TB/s read and written, a read stream 7.1): dispatch of 8192 tokens to 8 rows of 2048 each 51
+// us (6.0 TB/s), combine 52 (5.8), dispatch gradient 56 (6.0), combine gradient of 16384 x 4 99 (6.1); mix of 4096 x 2 rows of 14336
+// 79 (5.9), of 8192 x 8 rows of 1024 53 (5.0), their gradients 122 (5.8) and 81 (5.0). Rows of 2 KB at eight places of a
+// buffer are what costs there: one to four slots of that width move 5.6 TB/s, whatever their paths.
 #include "columns.h"
 
 namespace pcm {
@@ -204,8 +208,8 @@ hipError_t rows_by_slots(const RowsArgs& g, hipStream_t s) {
 
 template <class IN, class OUT, bool TO_ROWS>
 hipError_t rows_by_size(const RowsArgs& g, hipStream_t s) {
-    return streamed((g.R + (g.tokens ? g.T : 0)) * g.H * (int64_t)sizeof(IN)) ? rows_by_slots<IN, OUT, TO_ROWS, true>(g, s)
-                                                     : rows_by_slots<IN, OUT, TO_ROWS, false>(g, s);
+    const int64_t bytes = (g.R + (g.tokens ? g.T : 0)) * g.H * (int64_t)sizeof(IN);
+    return streamed(bytes) ? rows_by_slots<IN, OUT, TO_ROWS, true>(g, s) : rows_by_slots<IN, OUT, TO_ROWS, false>(g, s);
 }
 
 template <bool TO_ROWS>
@@ -293,7 +297,9 @@ __global__ __launch_bounds__(kThreads) void mix_rows_kernel(MixRowsArgs g) {
 
 // A wave takes A of a token's K sources, all targets and every per-th step of 64 C columns: A * K sums for dbeta in registers
 // next to the rows. All lanes of a wave stay active (past the last column on the last ones again, as zeros), so that the sums
-// cross the whole wave. Eight sources in one wave left two waves on a SIMD, waiting (8192 tokens, F 1024: 89 us; 2 x 4 SWEPT).
+// cross the whole wave. Eight sources in one wave left two waves on a SIMD, waiting (8192 tokens, F 1024: 89 us; two of four
+// sources 81; four of two 88). The products on the matrix cores instead, as a corner of X X^T of all a token's rows X, took 106: rows
+// in pieces of half a line, and dz a second time for du.
 template <class IN, class OUT, int K, int A, int C, bool STREAM>
 __global__ __launch_bounds__(kGradThreads) void mix_rows_grad_kernel(MixRowsArgs g, int per) {
     constexpr int N = pow2_above(A * K), kShares = (K + A - 1) / A;
@@ -421,8 +427,8 @@ hipError_t mix_by_slots(bool grad, const MixRowsArgs& g, hipStream_t s) {
 
 template <class IN, class OUT>
 hipError_t mix_by_size(bool grad, const MixRowsArgs& g, hipStream_t s) {
-    return streamed(((g.u ? g.R_src : 0) + (grad ? g.R_tgt : 0)) * g.F * (int64_t)sizeof(IN)) ? mix_by_slots<IN, OUT, true>(grad, g, s)
-                                                                           : mix_by_slots<IN, OUT, false>(grad, g, s);
+    const int64_t bytes = ((g.u ? g.R_src : 0) + (grad ? g.R_tgt : 0)) * g.F * (int64_t)sizeof(IN);
+    return streamed(bytes) ? mix_by_slots<IN, OUT, true>(grad, g, s) : mix_by_slots<IN, OUT, false>(grad, g, s);
 }
 
 }  // namespace
