@@ -410,9 +410,9 @@ pcm_status pcm_dispatch_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* x
                              int H, int n, void* y, void* stream);
 
 /* Its gradients: dx[t, :] = sum over a (ascending) of weights[t, a] dy[r, :], every row written; dweights[t, a] =
- * sum over the columns of dy[r, :] x[t, :], 0 for a pair without a row. dy [R,H] and x [T,H] of `dtype`, dx [T,H] of
- * out_dtype, dweights [T,k] f32. dx or dweights may be NULL: not wanted; x may be NULL without dweights. */
-pcm_status pcm_dispatch_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* x,
+ * sum over the columns of dy[r, :] x[t, :], 0 for a pair without a row. dy [R,H] of `dtype`, x [T,H] of x_dtype, dx [T,H]
+ * of out_dtype, dweights [T,k] f32. dx or dweights may be NULL: not wanted; x may be NULL without dweights. */
+pcm_status pcm_dispatch_rows_grad(pcm_dtype dtype, pcm_dtype x_dtype, pcm_dtype out_dtype, const void* dy, const void* x,
                                   const int32_t* row_of, const float* weights, const int32_t* offsets,
                                   int64_t T, int k, int64_t R, int H, int n, void* dx, float* dweights,
                                   void* stream);
@@ -424,9 +424,9 @@ pcm_status pcm_combine_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* o,
                             int H, int n, void* y, int accumulate, void* stream);
 
 /* Its gradients: d_o[r, :] = weights[t, a] dy[t, :], rows of no pair left as they were; dweights[t, a] = sum over
- * the columns of o[r, :] dy[t, :], 0 for a pair without a row. dy [T,H] and o [R,H] of `dtype`, d_o [R,H] of
+ * the columns of o[r, :] dy[t, :], 0 for a pair without a row. dy [T,H] of `dtype`, o [R,H] of o_dtype, d_o [R,H] of
  * out_dtype, dweights [T,k] f32. d_o or dweights may be NULL: not wanted; o may be NULL without dweights. */
-pcm_status pcm_combine_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* o,
+pcm_status pcm_combine_rows_grad(pcm_dtype dtype, pcm_dtype o_dtype, pcm_dtype out_dtype, const void* dy, const void* o,
                                  const int32_t* row_of, const float* weights, const int32_t* offsets,
                                  int64_t T, int k, int64_t R, int H, int n, void* d_o, float* dweights,
                                  void* stream);

@@ -131,7 +131,7 @@ def lib(path: str = _LIB_PATH) -> ctypes.CDLL:
     L.pcm_quant_fp8_weights.argtypes = [I, P, I, I, I, P, P, P, P, P]
     L.pcm_grouped_gemm_fp8.argtypes = [I, P, P, P, P, P, P, I64, I64, I, I, I, P, P]
     L.pcm_dispatch_rows.argtypes = [I, I, P, P, P, P, I64, I, I64, I, I, P, P]
-    L.pcm_dispatch_rows_grad.argtypes = [I, I, P, P, P, P, P, I64, I, I64, I, I, P, P, P]
+    L.pcm_dispatch_rows_grad.argtypes = [I, I, I, P, P, P, P, P, I64, I, I64, I, I, P, P, P]
     L.pcm_combine_rows.argtypes = [I, I, P, P, P, P, I64, I, I64, I, I, P, I, P]
     L.pcm_combine_rows_grad.argtypes = L.pcm_dispatch_rows_grad.argtypes
     L.pcm_swiglu.argtypes = [I, I, P, P, I64, I, P, P]

@@ -75,8 +75,8 @@ __device__ __forceinline__ void read(Raw<T, C>& r, const T* p) {
 // 39.8 / 42.3.
 inline bool streamed(int64_t bytes) { return bytes >= (int64_t)96 << 20; }
 // Columns a thread takes: 16 bytes of float32, where there is any, or of bf16, so that a wave's access is one piece.
-template <class IN, class OUT>
-constexpr int kCols = sizeof(IN) == 2 && sizeof(OUT) == 2 ? 8 : 4;
+template <class... T>
+constexpr int kCols = ((sizeof(T) == 2) && ...) ? 8 : 4;
 
 // C columns of a result, in float32; bf16 is rounded once, to nearest even. Results are stored non-temporally: they are
 // written once and read by a later kernel (dispatch of 8192 tokens to 8 rows of 2048 each 63 us -> 51).

@@ -304,7 +304,7 @@ struct RowsArgs {
     int accumulate;           // combine: add into out
     int parts;                // set by the launch: workgroups to a token's columns
 };
-hipError_t launch_rows(bool to_rows, bool bf16, bool out_bf16, const RowsArgs& g, hipStream_t s);
+hipError_t launch_rows(bool to_rows, bool tokens_bf16, bool rows_bf16, bool out_bf16, const RowsArgs& g, hipStream_t s);
 // The mix along a token's paths and its gradient.
 struct MixRowsArgs {
     const void* u;            // [R_src, F] (gradient: NULL where dbeta is not wanted)

@@ -958,12 +958,14 @@ pcm_status pcm_grouped_gemm_fp8(pcm_dtype out_dtype, const uint8_t* x, const flo
     return from_hip(launch_grouped_fp8(out_dtype == PCM_BF16, g, (hipStream_t)stream));
 }
 
-static pcm_status rows_call(bool to_rows, pcm_dtype dtype, pcm_dtype out_dtype, const void* tokens, const void* rows,
+static pcm_status rows_call(bool to_rows, pcm_dtype tokens_dtype, pcm_dtype rows_dtype, pcm_dtype out_dtype,
+                            const void* tokens, const void* rows,
                             const int32_t* row_of, const float* weights, const int32_t* offsets, int64_t T, int k,
                             int64_t R, int H, int n, void* out, float* dweights, bool dot, int accumulate, void* stream) {
     const pcm_status st = check_rows(T, R, k, H, n);
     if (st != PCM_OK) return st;
-    if (!plain_dtype(dtype) || !plain_dtype(out_dtype) || (!offsets && n != 1)) return PCM_ERR_ARG;
+    if (!plain_dtype(tokens_dtype) || !plain_dtype(rows_dtype) || !plain_dtype(out_dtype) || (!offsets && n != 1))
+        return PCM_ERR_ARG;
     if (accumulate && out_dtype != PCM_F32) return PCM_ERR_ARG;
     if (!aligned16(tokens) || !aligned16(rows) || !aligned16(row_of) || !aligned16(weights) || !aligned4(offsets) ||
         !aligned16(out) || !aligned16(dweights))
@@ -987,34 +989,35 @@ static pcm_status rows_call(bool to_rows, pcm_dtype dtype, pcm_dtype out_dtype, 
     g.H = H;
     g.n = n;
     g.accumulate = accumulate != 0;
-    return from_hip(launch_rows(to_rows, dtype == PCM_BF16, out_dtype == PCM_BF16, g, (hipStream_t)stream));
+    return from_hip(launch_rows(to_rows, tokens_dtype == PCM_BF16, rows_dtype == PCM_BF16, out_dtype == PCM_BF16, g,
+                                (hipStream_t)stream));
 }
 
 pcm_status pcm_dispatch_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* x, const int32_t* row_of,
                              const float* weights, const int32_t* offsets, int64_t T, int k, int64_t R,
                              int H, int n, void* y, void* stream) {
-    return rows_call(true, dtype, out_dtype, x, nullptr, row_of, weights, offsets, T, k, R, H, n, y, nullptr, false, 0, stream);
+    return rows_call(true, dtype, dtype, out_dtype, x, nullptr, row_of, weights, offsets, T, k, R, H, n, y, nullptr, false, 0, stream);
 }
 
-pcm_status pcm_dispatch_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* x,
+pcm_status pcm_dispatch_rows_grad(pcm_dtype dtype, pcm_dtype x_dtype, pcm_dtype out_dtype, const void* dy, const void* x,
                                   const int32_t* row_of, const float* weights, const int32_t* offsets,
                                   int64_t T, int k, int64_t R, int H, int n, void* dx, float* dweights,
                                   void* stream) {
-    return rows_call(false, dtype, out_dtype, x, dy, row_of, weights, offsets, T, k, R, H, n, dx, dweights, true, 0, stream);
+    return rows_call(false, x_dtype, dtype, out_dtype, x, dy, row_of, weights, offsets, T, k, R, H, n, dx, dweights, true, 0, stream);
 }
 
 pcm_status pcm_combine_rows(pcm_dtype dtype, pcm_dtype out_dtype, const void* o, const int32_t* row_of,
                             const float* weights, const int32_t* offsets, int64_t T, int k, int64_t R,
                             int H, int n, void* y, int accumulate, void* stream) {
-    return rows_call(false, dtype, out_dtype, nullptr, o, row_of, weights, offsets, T, k, R, H, n, y, nullptr, false, accumulate,
+    return rows_call(false, dtype, dtype, out_dtype, nullptr, o, row_of, weights, offsets, T, k, R, H, n, y, nullptr, false, accumulate,
                      stream);
 }
 
-pcm_status pcm_combine_rows_grad(pcm_dtype dtype, pcm_dtype out_dtype, const void* dy, const void* o,
+pcm_status pcm_combine_rows_grad(pcm_dtype dtype, pcm_dtype o_dtype, pcm_dtype out_dtype, const void* dy, const void* o,
                                  const int32_t* row_of, const float* weights, const int32_t* offsets,
                                  int64_t T, int k, int64_t R, int H, int n, void* d_o, float* dweights,
                                  void* stream) {
-    return rows_call(true, dtype, out_dtype, dy, o, row_of, weights, offsets, T, k, R, H, n, d_o, dweights, true, 0, stream);
+    return rows_call(true, dtype, o_dtype, out_dtype, dy, o, row_of, weights, offsets, T, k, R, H, n, d_o, dweights, true, 0, stream);
 }
 
 static pcm_status swiglu_call(pcm_dtype dtype, pcm_dtype out_dtype, const void* gate_up, const void* du, bool grad,

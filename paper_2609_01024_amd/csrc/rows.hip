@@ -11,6 +11,8 @@
 // us (6.0 TB/s), combine 52 (5.8), dispatch gradient 56 (6.0), combine gradient of 16384 x 4 99 (6.1); mix of 4096 x 2 rows of 14336
 // 79 (5.9), of 8192 x 8 rows of 1024 53 (5.0), their gradients 122 (5.8) and 81 (5.0). Rows of 2 KB at eight places of a
 // buffer are what costs there: one to four slots of that width move 5.6 TB/s, whatever their paths.
+#include <type_traits>
+
 #include "columns.h"
 
 namespace pcm {
@@ -89,12 +91,12 @@ __device__ __forceinline__ T* column(T* __restrict__ p, int64_t row, uint32_t c)
 
 // TO_ROWS: dispatch and the combine's gradient, from `tokens` to the rows of out; otherwise combine and the dispatch's
 // gradient, from `rows` to the tokens of out. DOT: dweights too, from both.
-template <class IN, class OUT, int KK, bool TO_ROWS, bool DOT, bool STREAM>
+template <class TOKEN, class ROW, class OUT, int KK, bool TO_ROWS, bool DOT, bool STREAM>
 __global__ __launch_bounds__(DOT ? kDotThreads<TO_ROWS> : kThreads) void rows_kernel(RowsArgs g) {
-    constexpr int C = kCols<IN, OUT>;
+    constexpr int C = kCols<TOKEN, ROW, OUT>;
     __shared__ float part[kDotThreads<TO_ROWS> / 64][KK];
-    const IN* __restrict__ tokens = (const IN*)g.tokens;
-    const IN* __restrict__ rows = (const IN*)g.rows;
+    const TOKEN* __restrict__ tokens = (const TOKEN*)g.tokens;
+    const ROW* __restrict__ rows = (const ROW*)g.rows;
     OUT* __restrict__ out = (OUT*)g.out;
     for (int64_t item = blockIdx.x; item < g.T * g.parts; item += gridDim.x) {
         const int64_t t = g.parts == 1 ? item : item / g.parts;
@@ -120,7 +122,8 @@ __global__ __launch_bounds__(DOT ? kDotThreads<TO_ROWS> : kThreads) void rows_ke
             r[a] = (int64_t)(on ? row[a] : first) * g.H;   // a row to read in any case, where there are any
         }
         for (int c = (part0 * blockDim.x + threadIdx.x) * C; c < g.H; c += g.parts * blockDim.x * C) {
-            Raw<IN, C> x, v[KK];
+            Raw<TOKEN, C> x;
+            Raw<ROW, C> v[KK];
             if (TO_ROWS || DOT) x.load(column(tokens, t * g.H, c));
             if ((!TO_ROWS || DOT) && held) {
 #pragma unroll
@@ -181,41 +184,47 @@ int threads_of(int64_t chunks, int parts, int most) {
     return (int)(share < most ? align_up(share, 64) : most);
 }
 
-template <class IN, class OUT, int KK, bool TO_ROWS, bool STREAM>
-hipError_t rows_by_dot(RowsArgs g, hipStream_t s) {
-    const int64_t chunks = g.H / kCols<IN, OUT>;
-    if (g.dweights) {
-        g.parts = 1;
-        const unsigned blocks = (unsigned)(g.T < kMostBlocks ? g.T : kMostBlocks);
-        const int threads = threads_of(chunks, (int)ceil_div(chunks, kDotThreads<TO_ROWS>), kDotThreads<TO_ROWS>);
-        rows_kernel<IN, OUT, KK, TO_ROWS, true, STREAM><<<dim3(blocks), threads, 0, s>>>(g);
-        return hipGetLastError();
-    }
-    g.parts = (int)ceil_div(chunks, kThreads);
+template <class TOKEN, class ROW, class OUT, int KK, bool TO_ROWS, bool DOT, bool STREAM>
+hipError_t rows_sized(RowsArgs g, hipStream_t s) {
+    const int64_t chunks = g.H / kCols<TOKEN, ROW, OUT>;
+    constexpr int kMost = DOT ? kDotThreads<TO_ROWS> : kThreads;
+    const int pieces = (int)ceil_div(chunks, kMost);      // passes of a workgroup, or workgroups
+    g.parts = DOT ? 1 : pieces;
     const int64_t items = g.T * g.parts;
-    const unsigned blocks = (unsigned)(items < kMostBlocks ? items : kMostBlocks);
-    rows_kernel<IN, OUT, KK, TO_ROWS, false, STREAM><<<dim3(blocks), threads_of(chunks, g.parts, kThreads), 0, s>>>(g);
+    rows_kernel<TOKEN, ROW, OUT, KK, TO_ROWS, DOT, STREAM>
+        <<<dim3((unsigned)(items < kMostBlocks ? items : kMostBlocks)), threads_of(chunks, pieces, kMost), 0, s>>>(g);
     return hipGetLastError();
 }
 
-template <class IN, class OUT, bool TO_ROWS, bool STREAM>
+template <class TOKEN, class ROW, class OUT, bool TO_ROWS, bool DOT, bool STREAM>
 hipError_t rows_by_slots(const RowsArgs& g, hipStream_t s) {
-    if (g.k <= 1) return rows_by_dot<IN, OUT, 1, TO_ROWS, STREAM>(g, s);
-    if (g.k <= 2) return rows_by_dot<IN, OUT, 2, TO_ROWS, STREAM>(g, s);
-    if (g.k <= 4) return rows_by_dot<IN, OUT, 4, TO_ROWS, STREAM>(g, s);
-    return rows_by_dot<IN, OUT, 8, TO_ROWS, STREAM>(g, s);
+    if (g.k <= 1) return rows_sized<TOKEN, ROW, OUT, 1, TO_ROWS, DOT, STREAM>(g, s);
+    if (g.k <= 2) return rows_sized<TOKEN, ROW, OUT, 2, TO_ROWS, DOT, STREAM>(g, s);
+    if (g.k <= 4) return rows_sized<TOKEN, ROW, OUT, 4, TO_ROWS, DOT, STREAM>(g, s);
+    return rows_sized<TOKEN, ROW, OUT, 8, TO_ROWS, DOT, STREAM>(g, s);
 }
 
-template <class IN, class OUT, bool TO_ROWS>
+template <class TOKEN, class ROW, class OUT, bool TO_ROWS, bool DOT>
 hipError_t rows_by_size(const RowsArgs& g, hipStream_t s) {
-    const int64_t bytes = (g.R + (g.tokens ? g.T : 0)) * g.H * (int64_t)sizeof(IN);
-    return streamed(bytes) ? rows_by_slots<IN, OUT, TO_ROWS, true>(g, s) : rows_by_slots<IN, OUT, TO_ROWS, false>(g, s);
+    // (towards the rows alone none are read)
+    if constexpr (TO_ROWS && !DOT) return rows_by_slots<TOKEN, ROW, OUT, TO_ROWS, DOT, false>(g, s);
+    else return streamed(g.R * g.H * (int64_t)sizeof(ROW) + (DOT ? g.T * g.H * (int64_t)sizeof(TOKEN) : 0))
+                    ? rows_by_slots<TOKEN, ROW, OUT, TO_ROWS, DOT, true>(g, s)
+                    : rows_by_slots<TOKEN, ROW, OUT, TO_ROWS, DOT, false>(g, s);
 }
 
-template <bool TO_ROWS>
-hipError_t rows_by_type(bool bf16, bool out_bf16, const RowsArgs& g, hipStream_t s) {
-    if (bf16) return out_bf16 ? rows_by_size<uint16_t, uint16_t, TO_ROWS>(g, s) : rows_by_size<uint16_t, float, TO_ROWS>(g, s);
-    return out_bf16 ? rows_by_size<float, uint16_t, TO_ROWS>(g, s) : rows_by_size<float, float, TO_ROWS>(g, s);
+// Without the products one side's rows are not read: its type is then the other's.
+template <class TOKEN, class ROW, class OUT, bool TO_ROWS>
+hipError_t rows_by_dot(const RowsArgs& g, hipStream_t s) {
+    using ONE = std::conditional_t<TO_ROWS, TOKEN, ROW>;
+    return g.dweights ? rows_by_size<TOKEN, ROW, OUT, TO_ROWS, true>(g, s) : rows_by_size<ONE, ONE, OUT, TO_ROWS, false>(g, s);
+}
+
+template <class OUT, bool TO_ROWS>
+hipError_t rows_by_type(bool tokens_bf16, bool rows_bf16, const RowsArgs& g, hipStream_t s) {
+    if (tokens_bf16)
+        return rows_bf16 ? rows_by_dot<uint16_t, uint16_t, OUT, TO_ROWS>(g, s) : rows_by_dot<uint16_t, float, OUT, TO_ROWS>(g, s);
+    return rows_bf16 ? rows_by_dot<float, uint16_t, OUT, TO_ROWS>(g, s) : rows_by_dot<float, float, OUT, TO_ROWS>(g, s);
 }
 
 // The token's paths: those whose two rows are there, and a row to read in any case (0 for a number that is no row; a
@@ -433,8 +442,10 @@ hipError_t mix_by_size(bool grad, const MixRowsArgs& g, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_rows(bool to_rows, bool bf16, bool out_bf16, const RowsArgs& g, hipStream_t s) {
-    return to_rows ? rows_by_type<true>(bf16, out_bf16, g, s) : rows_by_type<false>(bf16, out_bf16, g, s);
+hipError_t launch_rows(bool to_rows, bool tokens_bf16, bool rows_bf16, bool out_bf16, const RowsArgs& g, hipStream_t s) {
+    if (to_rows)
+        return out_bf16 ? rows_by_type<uint16_t, true>(tokens_bf16, rows_bf16, g, s) : rows_by_type<float, true>(tokens_bf16, rows_bf16, g, s);
+    return out_bf16 ? rows_by_type<uint16_t, false>(tokens_bf16, rows_bf16, g, s) : rows_by_type<float, false>(tokens_bf16, rows_bf16, g, s);
 }
 
 hipError_t launch_mix_rows(bool grad, bool bf16, bool out_bf16, const MixRowsArgs& g, hipStream_t s) {

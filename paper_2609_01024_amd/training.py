@@ -75,15 +75,15 @@ def pcm_dispatch_rows(x: torch.Tensor, row_of: torch.Tensor, weights=None, offse
 def pcm_dispatch_rows_grad(dy: torch.Tensor, row_of: torch.Tensor, x: Optional[torch.Tensor] = None, weights=None, offsets=None,
                            dx=None, dweights=None, out_dtype: Optional[torch.dtype] = None, stream=None):
     """(dx, dweights) of pcm_dispatch_rows: the sum of weights[t, a] dy[row_of[t, a]] over a token's slots, and, with x, the
-    products <dy[row_of[t, a]], x[t]> (None without)."""
+    products <dy[row_of[t, a]], x[t]> (None without). x may be of the other type."""
     R, H = _matrix(dy, "dy")
     _operand(dy, "dy")
     dev = dy.device
     T, k, n = _slots(row_of, weights, offsets, dev)
     out = _out_type(dx, out_dtype, dy.dtype)
-    dweights = _dots(x, "x", (T, H), dy.dtype, dweights, (T, k), dev, stream)
+    dweights = _dots(x, "x", (T, H), None, dweights, (T, k), dev, stream)
     dx = _out(dx, (T, H), out, dev, "dx", stream)
-    status = lib().pcm_dispatch_rows_grad(_code(dy.dtype), _code(out), _ptr(dy), _ptr(x), _ptr(row_of), _ptr(weights),
+    status = lib().pcm_dispatch_rows_grad(_code(dy.dtype), _code((dy if x is None else x).dtype), _code(out), _ptr(dy), _ptr(x), _ptr(row_of), _ptr(weights),
                                           _ptr(offsets), T, k, R, H, n, _ptr(dx), _ptr(dweights), _stream_on(stream, dev))
     if status:
         _check(status)
@@ -124,7 +124,7 @@ def pcm_combine_rows_grad(dy: torch.Tensor, row_of: torch.Tensor, o: Optional[to
                           stream=None):
     """(do, dweights) of pcm_combine_rows: do[row_of[t, a]] = weights[t, a] dy[t], and, with o, the products
     <o[row_of[t, a]], dy[t]> (None without). do has o's rows (or `rows`, T k by default); rows of no pair are left as
-    they were (in a `do` that the caller does not pass: undefined)."""
+    they were (in a `do` that the caller does not pass: undefined). o may be of the other type."""
     T, H = _matrix(dy, "dy")
     _operand(dy, "dy")
     dev = dy.device
@@ -135,9 +135,9 @@ def pcm_combine_rows_grad(dy: torch.Tensor, row_of: torch.Tensor, o: Optional[to
         rows = _row_count(rows, o, T, k)
     R = _row_count(rows, do, T, k)
     out = _out_type(do, out_dtype, dy.dtype)
-    dweights = _dots(o, "o", (R, H), dy.dtype, dweights, (T, k), dev, stream)
+    dweights = _dots(o, "o", (R, H), None, dweights, (T, k), dev, stream)
     do = _out(do, (R, H), out, dev, "do", stream)
-    status = lib().pcm_combine_rows_grad(_code(dy.dtype), _code(out), _ptr(dy), _ptr(o), _ptr(row_of), _ptr(weights),
+    status = lib().pcm_combine_rows_grad(_code(dy.dtype), _code((dy if o is None else o).dtype), _code(out), _ptr(dy), _ptr(o), _ptr(row_of), _ptr(weights),
                                          _ptr(offsets), T, k, R, H, n, _ptr(do), _ptr(dweights), _stream_on(stream, dev))
     if status:
         _check(status)

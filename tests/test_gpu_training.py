@@ -151,6 +151,45 @@ def test_combine_gradient(shape, types, held):
     same_bits(alone[gpu(on)], do[gpu(on)])
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,rows", [(BF, F32), (F32, BF)])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 16), (33, 2, 4, 2064), (70, 5, 9, 528), (3, 8, 8, 7168)])
+def test_row_gradients_of_two_types(shape, tokens, rows, out):
+    """Tokens of one type and rows of the other: a float32 gradient of outputs that were kept in bf16, and the other way."""
+    T, k, n, H = shape
+    out = {"bf16": BF, "f32": F32}[out]
+    c = tokens_and_rows(shape, F32, "all", 9)
+    x, o, of = c["x"].to(tokens), c["o"].to(rows), c["of"].long()
+    O, X, W = o.double()[of], x.double()[:, None, :], c["w"].double()[:, :, None]
+    dots, mag = (O * X).sum(2), (O * X).abs().sum(2)
+    do, dw = pcm.pcm_combine_rows_grad(gpu(x), gpu(c["of"]), gpu(o), gpu(c["w"]), out_dtype=out)
+    close(do[gpu(of)], X * W, U * (X * W).abs(), "do")
+    close(dw, dots, (H + 1) * U * mag, "dweights")
+    dx, dw = pcm.pcm_dispatch_rows_grad(gpu(o), gpu(c["of"]), gpu(x), gpu(c["w"]), out_dtype=out)
+    close(dx, (O * W).sum(1), (k + 1) * U * (O * W).abs().sum(1), "dx")
+    close(dw, dots, (H + 1) * U * mag, "dweights")
+
+
+def test_widest_rows():
+    """2^28 columns of small integers: a lane's sums stay below 2^24 and are exact, about ten additions after them round by
+    2^-24 each."""
+    H = 1 << 28
+    x = torch.ones((1, H), dtype=BF, device=DEV)
+    x[0, ::3] = 2.0
+    of, w = torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.full((1, 1), 4.0, device=DEV)
+    y = pcm.pcm_dispatch_rows(x, of, w)
+    assert torch.equal(y, 4 * x)
+    assert torch.equal(pcm.pcm_combine_rows(y, of, w), 16 * x)
+    bits = torch.ones(1, dtype=torch.int64, device=DEV)
+    assert torch.equal(pcm.pcm_mix_rows(x, bits, w[:, :, None].contiguous(), of), y)
+    twos = (H + 2) // 3
+    want = float(H - twos + 4 * twos)
+    dx, dw = pcm.pcm_dispatch_rows_grad(x, of, x, w)
+    assert torch.equal(dx, y) and abs(float(dw) - want) <= want * 2 ** -20
+    du, dbeta = pcm.pcm_mix_rows_grad(x, x, bits, w[:, :, None].contiguous(), of)
+    assert torch.equal(du, y) and abs(float(dbeta) - want) <= want * 2 ** -20
+
+
 @pytest.mark.parametrize("types", ["bf16-f32", "f32-f32"])
 def test_row_gradients_against_differences(types):
     """<dy, f(v + d) - f(v - d)> = 2 <df, d> in each argument, which the operators are linear in. Small integers and
@@ -236,11 +275,11 @@ def test_products_alone(types, H):
     x, o, of, w, bits, beta, u, dz = (gpu(v) for v in (c["x"], c["o"], c["of"], c["w"], m["bits"], m["beta"], m["u"], m["dz"]))
     got = torch.full((T, k), 7.0, device=DEV)
     L, P, R = pcm.lib(), torch.Tensor.data_ptr, T * k
-    assert L.pcm_dispatch_rows_grad(code, 0, P(o), P(x), P(of), P(w), None, T, k, R, H, 1, None, P(got), None) == 0
+    assert L.pcm_dispatch_rows_grad(code, code, 0, P(o), P(x), P(of), P(w), None, T, k, R, H, 1, None, P(got), None) == 0
     torch.cuda.synchronize()
     same_bits(got, pcm.pcm_dispatch_rows_grad(o, of, x, w, out_dtype=F32)[1])
     got.fill_(7.0)
-    assert L.pcm_combine_rows_grad(code, 0, P(x), P(o), P(of), P(w), None, T, k, R, H, 1, None, P(got), None) == 0
+    assert L.pcm_combine_rows_grad(code, code, 0, P(x), P(o), P(of), P(w), None, T, k, R, H, 1, None, P(got), None) == 0
     torch.cuda.synchronize()
     same_bits(got, pcm.pcm_combine_rows_grad(x, of, o, w, out_dtype=F32)[1])
     got = torch.full((T, k, k), 7.0, device=DEV)
@@ -907,7 +946,7 @@ def test_refuses_tensors_the_kernels_must_not_address():
         with pytest.raises(ValueError):
             call()
     for call in (lambda: pcm.pcm_dispatch_rows(x, of.long()), lambda: pcm.pcm_dispatch_rows(x, of, w.double()),
-                 lambda: pcm.pcm_dispatch_rows(x.half(), of), lambda: pcm.pcm_dispatch_rows_grad(o, of, x.float()),
+                 lambda: pcm.pcm_dispatch_rows(x.half(), of), lambda: pcm.pcm_dispatch_rows_grad(o, of, x.half()),
                  lambda: pcm.pcm_combine_rows(o, of, out_dtype=torch.float16), lambda: pcm.pcm_swiglu_grad(o, o[:, :272].float()),
                  lambda: pcm.pcm_mix_rows(o, bits.int(), beta, of), lambda: pcm.pcm_mix_rows_grad(o, o.float(), bits, beta, of),
                  lambda: pcm.pcm_route_grad(c["ids"], w.bfloat16(), 16, dw=w)):

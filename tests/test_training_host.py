@@ -25,16 +25,16 @@ def dispatch(dt=BF16, out=BF16, x=P, of=P, w=P, off=P, T=8, k=2, R=16, H=64, n=4
     return (dt, out, x, of, w, off, T, k, R, H, n, y, None)
 
 
-def dispatch_grad(dt=BF16, out=BF16, dy=P, x=P, of=P, w=P, off=P, T=8, k=2, R=16, H=64, n=4, dx=P, dw=P):
-    return (dt, out, dy, x, of, w, off, T, k, R, H, n, dx, dw, None)
+def dispatch_grad(dt=BF16, other=F32, out=BF16, dy=P, x=P, of=P, w=P, off=P, T=8, k=2, R=16, H=64, n=4, dx=P, dw=P):
+    return (dt, other, out, dy, x, of, w, off, T, k, R, H, n, dx, dw, None)
 
 
 def combine(dt=BF16, out=BF16, o=P, of=P, w=P, off=P, T=8, k=2, R=16, H=64, n=4, y=P, acc=0):
     return (dt, out, o, of, w, off, T, k, R, H, n, y, acc, None)
 
 
-def combine_grad(dt=BF16, out=BF16, dy=P, o=P, of=P, w=P, off=P, T=8, k=2, R=16, H=64, n=4, do=P, dw=P):
-    return (dt, out, dy, o, of, w, off, T, k, R, H, n, do, dw, None)
+def combine_grad(dt=BF16, other=F32, out=BF16, dy=P, o=P, of=P, w=P, off=P, T=8, k=2, R=16, H=64, n=4, do=P, dw=P):
+    return (dt, other, out, dy, o, of, w, off, T, k, R, H, n, do, dw, None)
 
 
 def mix(dt=BF16, out=BF16, u=P, bits=P, beta=P, src=P, tgt=P, T=8, k=2, R=16, R_tgt=16, H=64, z=P):
@@ -70,6 +70,8 @@ def test_sizes_and_types(L, name):
     if name in ON_TOKENS:
         for bad, want in ((dict(T=-1), ARG), (dict(k=0), ARG), (dict(k=9), UNSUP), (dict(T=1 << 30), UNSUP)):
             assert call(*args(**bad)) == want, (name, bad)
+    if name in ("pcm_dispatch_rows_grad", "pcm_combine_rows_grad"):
+        assert call(*args(other=F16DOWN)) == ARG and call(*args(other=-1)) == ARG
     if name in ON_GROUPS:
         for bad, want in ((dict(n=0), ARG), (dict(n=257), UNSUP), (dict(off=None), ARG)):
             assert call(*args(**bad)) == want, (name, bad)
