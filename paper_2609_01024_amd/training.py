@@ -301,10 +301,15 @@ def _device(tensors):
     return tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
 
 
-def _one(norm, device, stream):
-    if norm is not None and norm.numel() != 1:
+def _one(norm, device):
+    if norm.numel() != 1:
         raise ValueError("norm must be one number")
-    return _out(norm, (1,) if norm is None else norm.shape, _F32, device, "norm", stream)
+    _operand(norm, "norm", _F32, None, device)
+    return norm
+
+
+def _norm_out(norm, device, stream):
+    return _out(None, (1,), _F32, device, "norm", stream) if norm is None else _one(norm, device)
 
 
 def pcm_grad_norm(grads: Sequence[torch.Tensor], norm=None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -313,7 +318,7 @@ def pcm_grad_norm(grads: Sequence[torch.Tensor], norm=None, ws: Optional[torch.T
     grads = list(grads)
     words, _ = _tensors(grads, "grads")
     dev = _device(grads)
-    norm = _one(norm, dev, stream)
+    norm = _norm_out(norm, dev, stream)
     ws = _workspace(ws, workspace_bytes(OP_GRAD_NORM, len(grads), 0, 0, 1, 1, 0), dev, stream)
     status = lib().pcm_grad_norm(_address(words), len(grads), _ptr(norm), _ptr(ws), ws.numel(), _stream_on(stream, dev))
     if status:
@@ -325,9 +330,11 @@ def pcm_clip_grads(grads: Sequence[torch.Tensor], norm: torch.Tensor, max_norm: 
     """Where norm (one float32 on the device) is over max_norm, the gradients times max_norm / norm; as they are where it is
     not, or is not finite. In place, or into the tensors of `out` (of either type). Gradients must not overlap. Returns
     out, or grads."""
+    if norm is None:
+        raise ValueError("norm must be given: pcm_clip_grad_norm forms it")
     clipped, grads, out = grads if out is None else out, list(grads), None if out is None else list(out)
     words, to, dev = _clipped(grads, out)
-    norm = _one(norm, dev, stream)
+    _one(norm, dev)
     status = lib().pcm_clip_grads(_address(words), _address(to), len(grads), _ptr(norm), float(max_norm),
                                   _stream_on(stream, dev))
     if status:
@@ -340,7 +347,7 @@ def pcm_clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out=None,
     """pcm_grad_norm and pcm_clip_grads with that norm, the same results; returns the norm."""
     grads = list(grads)
     words, to, dev = _clipped(grads, None if out is None else list(out))
-    norm = _one(norm, dev, stream)
+    norm = _norm_out(norm, dev, stream)
     ws = _workspace(ws, workspace_bytes(OP_GRAD_NORM, len(grads), 0, 0, 1, 1, 0), dev, stream)
     status = lib().pcm_clip_grad_norm(_address(words), _address(to), len(grads), float(max_norm), _ptr(norm),
                                       _ptr(ws), ws.numel(), _stream_on(stream, dev))

@@ -227,3 +227,9 @@ def test_python_refuses_sizes_past_32_bits():
                  lambda: pcm.pcm_mix_rows_grad(x, x, of, of, of), lambda: pcm.pcm_route_grad(x.int(), x, 8)):
         with pytest.raises(ValueError, match="32 bits"):
             call()
+
+
+def test_python_clips_by_a_norm_that_is_given():
+    """The norm is an input: it cannot be left out."""
+    with pytest.raises(ValueError, match="norm"):
+        pcm.pcm_clip_grads([torch.zeros(4)], None, 1.0)
