@@ -286,6 +286,11 @@ def _address(words: Optional[array]):
     return words.buffer_info()[0] if words else None
 
 
+def _listed(tensors):
+    """What can be read more than once: an iterator would come back empty."""
+    return tensors if isinstance(tensors, (list, tuple)) else list(tensors)
+
+
 def _clipped(grads, out):
     """The arrays of grads and of out (None in place), and their device."""
     words, counts = _tensors(grads, "grads")
@@ -329,17 +334,17 @@ def pcm_grad_norm(grads: Sequence[torch.Tensor], norm=None, ws: Optional[torch.T
 def pcm_clip_grads(grads: Sequence[torch.Tensor], norm: torch.Tensor, max_norm: float, out=None, stream=None):
     """Where norm (one float32 on the device) is over max_norm, the gradients times max_norm / norm; as they are where it is
     not, or is not finite. In place, or into the tensors of `out` (of either type). Gradients must not overlap. Returns
-    out, or grads."""
+    out, or grads: the list or tuple itself, of another iterable a list."""
     if norm is None:
         raise ValueError("norm must be given: pcm_clip_grad_norm forms it")
-    clipped, grads, out = grads if out is None else out, list(grads), None if out is None else list(out)
+    grads, out = _listed(grads), None if out is None else _listed(out)
     words, to, dev = _clipped(grads, out)
     _one(norm, dev)
     status = lib().pcm_clip_grads(_address(words), _address(to), len(grads), _ptr(norm), float(max_norm),
                                   _stream_on(stream, dev))
     if status:
         _check(status)
-    return clipped
+    return grads if out is None else out
 
 
 def pcm_clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out=None, norm=None, ws: Optional[torch.Tensor] = None,

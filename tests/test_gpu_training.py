@@ -808,6 +808,18 @@ def test_clip_by_a_norm_of_several_ranks():
     assert pcm.pcm_clip_grads(grads, norm, float("inf")) is grads and torch.equal(grads[0], want)
 
 
+def test_clip_of_what_can_be_read_once():
+    """Gradients and results from generators come back as lists that hold them; a list comes back itself."""
+    norm = torch.tensor(8.0, device=DEV)
+    grads = [torch.full((n,), 4.0, device=DEV) for n in (5, 300)]
+    outs = [torch.zeros_like(g) for g in grads]
+    back = list(pcm.pcm_clip_grads((g for g in grads), norm, 2.0, out=(o for o in outs)))
+    assert len(back) == 2 and all(b is o for b, o in zip(back, outs)) and all(bool((o == 1.0).all()) for o in outs)
+    back = list(pcm.pcm_clip_grads(iter(grads), norm, 2.0))
+    assert len(back) == 2 and all(b is g for b, g in zip(back, grads)) and all(bool((g == 1.0).all()) for g in grads)
+    assert pcm.pcm_clip_grads(grads, norm, 100.0, out=outs) is outs
+
+
 def test_norm_of_nothing():
     assert float(pcm.pcm_grad_norm([])) == 0.0
     assert float(pcm.pcm_clip_grad_norm([], 1.0)) == 0.0
