@@ -820,6 +820,29 @@ def test_clip_of_what_can_be_read_once():
     assert pcm.pcm_clip_grads(grads, norm, 100.0, out=outs) is outs
 
 
+@pytest.mark.parametrize("count", [512, 513, 1024, 1025, 4096])
+def test_clip_of_many_tensors(count):
+    """Up to the most a call takes, in place and into others, in an order that is not that of their addresses."""
+    g = torch.Generator().manual_seed(count)
+    flat = torch.randn(count * 5, generator=g)
+    order = torch.randperm(count, generator=g).tolist()
+    here, there = gpu(flat), torch.full((count * 5,), 7.0, dtype=BF, device=DEV)
+    grads, outs = [here[5 * i:5 * i + 1 + i % 5] for i in order], [there[5 * i:5 * i + 1 + i % 5] for i in order]
+    host = [v.cpu() for v in grads]
+    want = norm64(host)
+    norm = pcm.pcm_clip_grad_norm(grads, 1.0, out=outs)
+    assert abs(float(norm) - want) <= 2 * U * want
+    written = torch.zeros(count * 5, dtype=torch.bool)
+    for i in order:
+        written[5 * i:5 * i + 1 + i % 5] = True
+    value = flat.double() / want
+    close(there[gpu(written)], value[written], 4 * U * value[written].abs(), "out")
+    assert bool((there[gpu(~written)] == 7.0).all())
+    pcm.pcm_clip_grads(grads, norm, 1.0)
+    close(here[gpu(written)], value[written], 4 * U * value[written].abs(), "in place")
+    same_bits(here[gpu(~written)], flat[~written])
+
+
 def test_norm_of_nothing():
     assert float(pcm.pcm_grad_norm([])) == 0.0
     assert float(pcm.pcm_clip_grad_norm([], 1.0)) == 0.0
