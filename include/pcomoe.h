@@ -478,7 +478,8 @@ typedef struct pcm_tensor {
 /* The norm over all gradients: norm [1] f32 (device) = sqrt(sum of squares of every element of grads[0, m)), squares and
  * sums in 64 bits, the norm rounded (over float32's largest: infinite). `grads` is host memory, read before the
  * call returns; m <= 4096.
- * ws: pcm_workspace_bytes(PCM_OP_GRAD_NORM, m, 0, 0, 1, 1, 0) bytes. Calls that overlap in time must not share it. */
+ * ws: pcm_workspace_bytes(PCM_OP_GRAD_NORM, m, 0, 0, 1, 1, 0) bytes. Calls that overlap in time must not share it. norm
+ * and ws lie on no tensor of a call and not on each other; the norm that pcm_clip_grads reads, on none that it writes. */
 pcm_status pcm_grad_norm(const pcm_tensor* grads, int m, float* norm, void* ws, size_t ws_bytes, void* stream);
 
 /* Clipping by a norm on the device (pcm_grad_norm's, or one made of several ranks'): with norm > max_norm, out[i] =

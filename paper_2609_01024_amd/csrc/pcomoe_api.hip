@@ -140,6 +140,16 @@ bool overlapping(const pcm_tensor* in, const pcm_tensor* out, int m) {
     each([&](uint16_t i) { s.numbers[count++] = i; });
     return any_shared(s.numbers, count, [=](uint16_t i) { return range_of(tensor(i)); });
 }
+// Whether `bytes` at p share memory with a tensor of a call.
+bool on_tensors(const pcm_tensor* in, const pcm_tensor* out, int m, const void* p, size_t bytes) {
+    const uintptr_t from = (uintptr_t)p, to = from + bytes;
+    for (const pcm_tensor* t : {in, out})
+        for (int i = 0; t && i < m; ++i) {
+            const Range r = range_of(t[i]);
+            if (t[i].count && r.from < to && from < r.to) return true;
+        }
+    return false;
+}
 pcm_status check_clip(const pcm_tensor* grads, const pcm_tensor* out, int m, float max_norm) {
     if (m < 0 || !(max_norm >= 0.0f)) return PCM_ERR_ARG;
     if (m > kMaxTensors) return PCM_ERR_UNSUPPORTED;
@@ -1135,17 +1145,22 @@ pcm_status pcm_route_grad(pcm_dtype out_dtype, const int32_t* topk_ids, const fl
     return from_hip(launch_route_grad(out_dtype == PCM_BF16, g, (hipStream_t)stream));
 }
 
-static pcm_status check_norm(int m, const float* norm, const void* ws, size_t ws_bytes) {
+static pcm_status check_norm(const pcm_tensor* grads, const pcm_tensor* out, int m, const float* norm, const void* ws,
+                             size_t ws_bytes) {
     if (!norm || !aligned4(norm)) return PCM_ERR_ARG;
-    if (ws_bytes < pcm_workspace_bytes(PCM_OP_GRAD_NORM, m, 0, 0, 1, 1, PCM_F32) || !ws) return PCM_ERR_WORKSPACE;
-    return aligned16(ws) ? PCM_OK : PCM_ERR_ARG;
+    const size_t need = pcm_workspace_bytes(PCM_OP_GRAD_NORM, m, 0, 0, 1, 1, PCM_F32);
+    if (ws_bytes < need || !ws) return PCM_ERR_WORKSPACE;
+    if (!aligned16(ws)) return PCM_ERR_ARG;
+    const uintptr_t in_ws = (uintptr_t)norm - (uintptr_t)ws;
+    if (in_ws < need || on_tensors(grads, out, m, norm, sizeof(float)) || on_tensors(grads, out, m, ws, need)) return PCM_ERR_ARG;
+    return PCM_OK;
 }
 
 pcm_status pcm_grad_norm(const pcm_tensor* grads, int m, float* norm, void* ws, size_t ws_bytes, void* stream) {
     if (m < 0 || (m && !grads)) return PCM_ERR_ARG;
     if (m > kMaxTensors) return PCM_ERR_UNSUPPORTED;
     pcm_status st = check_tensors(grads, m);
-    if (st == PCM_OK) st = check_norm(m, norm, ws, ws_bytes);
+    if (st == PCM_OK) st = check_norm(grads, nullptr, m, norm, ws, ws_bytes);
     if (st != PCM_OK) return st;
     return from_hip(launch_grad_norm(grads, nullptr, m, false, 0.0f, norm, (double*)ws, (hipStream_t)stream));
 }
@@ -1155,14 +1170,14 @@ pcm_status pcm_clip_grads(const pcm_tensor* grads, const pcm_tensor* out, int m,
     const pcm_status st = check_clip(grads, out, m, max_norm);
     if (st != PCM_OK) return st;
     if (m == 0) return PCM_OK;
-    if (!norm || !aligned4(norm)) return PCM_ERR_ARG;
+    if (!norm || !aligned4(norm) || on_tensors(out ? out : grads, nullptr, m, norm, sizeof(float))) return PCM_ERR_ARG;
     return from_hip(launch_grad_norm(grads, out, m, true, max_norm, (float*)norm, nullptr, (hipStream_t)stream));
 }
 
 pcm_status pcm_clip_grad_norm(const pcm_tensor* grads, const pcm_tensor* out, int m, float max_norm,
                               float* norm, void* ws, size_t ws_bytes, void* stream) {
     pcm_status st = check_clip(grads, out, m, max_norm);
-    if (st == PCM_OK) st = check_norm(m, norm, ws, ws_bytes);
+    if (st == PCM_OK) st = check_norm(grads, out, m, norm, ws, ws_bytes);
     if (st != PCM_OK) return st;
     return from_hip(launch_grad_norm(grads, out, m, true, max_norm, norm, (double*)ws, (hipStream_t)stream));
 }

@@ -843,6 +843,24 @@ def test_clip_of_many_tensors(count):
     same_bits(here[gpu(~written)], flat[~written])
 
 
+def test_norm_beside_the_gradients():
+    """The norm next to a gradient in one buffer; one of the gradients where only results are written; never on a written one."""
+    flat = torch.full((100,), 2.0, device=DEV)
+    grads, norm = [flat[1:60], flat[61:]], flat[60:61]
+    assert pcm.pcm_clip_grad_norm(grads, 1.0, norm=norm) is norm
+    want = 2.0 * math.sqrt(98)
+    assert abs(float(norm) - want) <= 2 * U * want and float(flat[0]) == 2.0
+    close(torch.cat(grads), torch.full((98,), 2.0 / want, dtype=torch.float64), 4 * U * torch.full((98,), 2.0 / want, dtype=torch.float64))
+    flat.fill_(2.0)
+    out = pcm.pcm_clip_grads([flat[:50]], flat[:1], 1.0, out=[torch.zeros(50, device=DEV)])
+    assert bool((out[0] == 1.0).all())
+    for call in (lambda: pcm.pcm_clip_grads([flat[:50]], flat[49:50], 1.0), lambda: pcm.pcm_grad_norm([flat[:50]], norm=flat[7:8]),
+                 lambda: pcm.pcm_clip_grad_norm([flat[:50]], 1.0, norm=flat[:1])):
+        with pytest.raises(RuntimeError):
+            call()
+    assert bool((flat == 2.0).all())
+
+
 def test_norm_of_nothing():
     assert float(pcm.pcm_grad_norm([])) == 0.0
     assert float(pcm.pcm_clip_grad_norm([], 1.0)) == 0.0

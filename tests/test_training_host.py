@@ -258,3 +258,25 @@ def test_clip_checks_on_a_small_stack():
     from paper_2609_01024_amd import build
     r = subprocess.run([sys.executable, "-c", SMALL_STACK, build.LIB], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0 and r.stdout.strip() == f"status [{ARG}]", (r.returncode, r.stdout, r.stderr[-500:])
+
+
+def test_norm_and_workspace_apart_from_the_tensors(L):
+    """The norm and the sums behind it on a gradient or a result: read by some workgroups after others wrote there."""
+    need = binding.workspace_bytes(binding.OP_GRAD_NORM, 2, 0, 0, 1, 1, 0)
+    far, more = ctypes.c_void_p(0x900000), [(0x30000, 64, BF16), (0x40000, 64, F32)]
+    on = [0x10000, 0x10000 + 252, 0x20000, 0x20000 + 124]      # first and last elements of A and B
+    for p in on:
+        norm = ctypes.c_void_p(p)
+        assert L.pcm_grad_norm(tensors(A, B), 2, norm, far, need, None) == ARG, hex(p)
+        assert clip(L, [A, B], norm=norm, ws=far) == {ARG}, hex(p)
+        assert L.pcm_clip_grad_norm(tensors(A, B), tensors(*more), 2, 1.0, norm, far, need, None) == ARG, hex(p)
+        assert clip(L, more, out=[B, A], norm=norm, ws=far) == {ARG}, hex(p)
+    for p in (0x10000, 0x10000 - need + 16, 0x20000 + 112):
+        ws, norm = ctypes.c_void_p(p), ctypes.c_void_p(0x990000)
+        assert L.pcm_grad_norm(tensors(A, B), 2, norm, ws, need, None) == ARG, hex(p)
+        assert L.pcm_clip_grad_norm(tensors(A, B), None, 2, 1.0, norm, ws, need, None) == ARG, hex(p)
+        assert L.pcm_clip_grad_norm(tensors(*more), tensors(B, A), 2, 1.0, norm, ws, need, None) == ARG, hex(p)
+    for p in (0x900000, 0x900000 + need - 4):                  # the norm in the workspace
+        norm = ctypes.c_void_p(p)
+        assert L.pcm_grad_norm(tensors(A, B), 2, norm, far, need, None) == ARG
+        assert L.pcm_clip_grad_norm(tensors(A, B), None, 2, 1.0, norm, far, need, None) == ARG
