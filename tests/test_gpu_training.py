@@ -337,6 +337,69 @@ def test_many_tokens():
     assert torch.equal(d[:, 0], 0.25 * dots[:, 0]) and not bool(d[:, 1:].any())
 
 
+# From 96 MB read on the kernels load non-temporally: the same at few tokens whose rows lie anywhere in buffers of that size.
+LARGE = 96 << 20
+
+
+def rows_in_a_large_buffer(T, k, H, dtype, seed):
+    """(R, of [T, k]) of rows spread over a buffer of at least LARGE bytes, the first and last ones among them."""
+    R = LARGE // (H * (2 if dtype == BF else 4)) + 1
+    g = torch.Generator().manual_seed(seed)
+    at = torch.randperm(R, generator=g)[:T * k]
+    if T * k > 1:
+        at[at == 0], at[at == R - 1] = at[0].item(), at[-1].item()
+        at[0], at[-1] = 0, R - 1
+    assert at.unique().numel() == T * k
+    return R, at.reshape(T, k).int()
+
+
+def in_a_large_buffer(R, of, v, fill=float("nan")):
+    """[R, H], `fill` but for the rows v [T, k, H] of `of`."""
+    o = torch.full((R, v.shape[-1]), fill, dtype=v.dtype, device=DEV)
+    o[gpu(of.reshape(-1).long())] = gpu(v.reshape(-1, v.shape[-1]))
+    return o
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,rows", [(BF, BF), (F32, F32), (BF, F32), (F32, BF)], ids=str)
+@pytest.mark.parametrize("k,H", [(1, 2064), (2, 208), (3, 2064), (4, 528), (5, 208), (8, 2064)])
+def test_rows_of_large_buffers(k, H, tokens, rows, out):
+    T, out = 37, {"bf16": BF, "f32": F32}[out]
+    R, of = rows_in_a_large_buffer(T, k, H, rows, k)
+    g = torch.Generator().manual_seed(k + 1)
+    x, v, w = torch.randn((T, H), generator=g).to(tokens), torch.randn((T, k, H), generator=g).to(rows), torch.rand((T, k), generator=g)
+    o = in_a_large_buffer(R, of, v)
+    X, V, W = x.double()[:, None, :], v.double(), w.double()[:, :, None]
+    want, room = (V * W).sum(1), (k + 1) * U * (V * W).abs().sum(1)
+    dots, dots_room = (V * X).sum(2), (H + 1) * U * (V * X).abs().sum(2)
+    if tokens == rows:
+        close(pcm.pcm_combine_rows(o, gpu(of), gpu(w), out_dtype=out), want, room, "y")
+    dx, dw = pcm.pcm_dispatch_rows_grad(o, gpu(of), gpu(x), gpu(w), out_dtype=out)
+    close(dx, want, room, "dx")
+    close(dw, dots, dots_room, "dweights")
+    do, dw = pcm.pcm_combine_rows_grad(gpu(x), gpu(of), o, gpu(w), do=torch.full((R, H), 7.0, dtype=out, device=DEV))
+    close(do[gpu(of.long())], X * W, U * (X * W).abs(), "do")
+    close(dw, dots, dots_room, "dweights")
+    do[gpu(of.reshape(-1).long())] = 7.0
+    assert bool((do == 7.0).all())
+
+
+def test_training_sized_row_gradients():
+    """Every token of a large batch, four rows each; the products of small integers are exact in float32."""
+    T, k, H = 16_384, 4, 1040
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randint(-3, 4, (T, H), generator=g, device=DEV).to(BF)
+    o = torch.randint(-3, 4, (T * k, H), generator=g, device=DEV).to(BF)
+    of = torch.randperm(T * k, generator=g, device=DEV).reshape(T, k).int()
+    w = torch.randint(1, 4, (T, k), generator=g, device=DEV).float() / 4
+    rows = o[of.long()].float()
+    dots = (rows * x.float()[:, None, :]).sum(2)
+    do, dw = pcm.pcm_combine_rows_grad(x, of, o, w, out_dtype=F32)
+    assert torch.equal(do[of.long()], x.float()[:, None, :] * w[:, :, None]) and torch.equal(dw, dots)
+    dx, dw = pcm.pcm_dispatch_rows_grad(o, of, x, w, out_dtype=F32)
+    assert torch.equal(dx, (rows * w[:, :, None]).sum(1)) and torch.equal(dw, dots)
+
+
 def test_no_tokens_and_no_rows():
     e = lambda *s, dt=F32: torch.empty(s, dtype=dt, device=DEV)
     i = lambda *s: torch.empty(s, dtype=torch.int32, device=DEV)
@@ -487,6 +550,26 @@ def test_swiglu_past_32_bits():
     assert not bool(u[:-40].any()) and not bool(d[:100].any())
 
 
+@pytest.mark.parametrize("types", TYPES)
+def test_swiglu_of_many_rows(types):
+    """From 96 MB read on, every element, in 64 bits on the card."""
+    dt, out = TYPES[types]
+    F = 1040
+    R = LARGE // (2 * F * (2 if dt == BF else 4)) + 3
+    g = torch.Generator(device=DEV).manual_seed(2)
+    gu, du = (torch.randn((R, n), generator=g, device=DEV, dtype=dt) * 3 for n in (2 * F, F))
+    gate, up, d = gu[:, :F].double(), gu[:, F:].double(), du.double()
+
+    def near(got, want, room, what):       # close(), where the tensors are
+        half = 2.0 ** -8 if got.dtype == BF else 0.0
+        bad = ~((got.double() - want).abs() <= room + half * (want.abs() + room) + 2.0 ** -134)
+        assert got.shape == want.shape and not bool(bad.any()), (what, int(bad.sum()))
+
+    want = swiglu64(gate, up)
+    near(pcm.pcm_swiglu(gu, out_dtype=out), want, swiglu_room(gate, up, want), "u")
+    near(pcm.pcm_swiglu_grad(gu, du, out_dtype=out), swiglu_grads64(gate, up, d), swiglu_grad_room(gate, up, d), "dgate_up")
+
+
 # ------------------------------------------------------------------------ mix along the paths
 def path_case(T, k, n, F, dtype, density, seed=0):
     c = routed(T, k, n, seed)
@@ -584,6 +667,36 @@ def test_mix_on_scored_tables(K):
     c["u"], c["dz"] = torch.randn((T * K, F), generator=g).to(BF), torch.randn((T * K, F), generator=g).to(BF)
     assert bool((c["src"] < 0).any()) and bool((c["tgt"] < 0).any())
     check_mix(c, F32, c["src"] >= 0, c["tgt"] >= 0)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("k,F", [(1, 2064), (2, 208), (3, 528), (4, 2064), (5, 272), (6, 80), (7, 1040), (8, 2064)])
+def test_mix_of_large_buffers(k, F, types):
+    """From 96 MB read on the mixes load non-temporally; the gradient of more than four slots one of its operands."""
+    dt, out = TYPES[types]
+    T = 29
+    c = path_case(T, k, 11, F, dt, 0.4, seed=k)
+    R, src = rows_in_a_large_buffer(T, k, F, dt, k)
+    tgt = rows_in_a_large_buffer(T, k, F, dt, k + 50)[1]
+    u, dz = c["u"].reshape(T, k, F), c["dz"].reshape(T, k, F)
+    beta = torch.where(c["on"], c["beta"], float("nan"))
+    B, U64, D64 = torch.where(c["on"], c["beta"].double(), 0.0), u.double(), dz.double()
+    args = gpu(c["bits"]), gpu(beta), gpu(src), gpu(tgt)
+    ub, db = in_a_large_buffer(R, src, u), in_a_large_buffer(R, tgt, dz)
+    z = pcm.pcm_mix_rows(ub, *args, z=torch.full((R, F), 7.0, dtype=out, device=DEV))
+    close(z[gpu(tgt.long())], torch.matmul(B.mT, U64), (k + 1) * U * torch.matmul(B.mT, U64.abs()), "z")
+    z[gpu(tgt.reshape(-1).long())] = 7.0
+    assert bool((z == 7.0).all())
+    du, dbeta = pcm.pcm_mix_rows_grad(db, ub, *args, du=torch.full((R, F), 7.0, dtype=out, device=DEV))
+    room = (k + 1) * U * torch.matmul(B, D64.abs())
+    close(du[gpu(src.long())], torch.matmul(B, D64), room, "du")
+    close(dbeta, torch.where(c["on"], torch.matmul(U64, D64.mT), 0.0), (F + 1) * U * torch.matmul(U64.abs(), D64.abs().mT), "dbeta")
+    alone, nothing = pcm.pcm_mix_rows_grad(db, None, *args, rows=R, du=torch.full((R, F), 7.0, dtype=out, device=DEV))
+    assert nothing is None
+    close(alone[gpu(src.long())], torch.matmul(B, D64), room, "du alone")
+    for d in (du, alone):
+        d[gpu(src.reshape(-1).long())] = 7.0
+        assert bool((d == 7.0).all())
 
 
 @pytest.mark.parametrize("types", ["bf16-f32", "f32-f32"])
