@@ -1205,3 +1205,44 @@ def test_training_step_with_dispatch_and_weights():
     assert drows.shape == (T * k, F)
     dx, _ = pcm.pcm_dispatch_rows_grad(rows, of)
     close(dx, k * x.double(), 0 * x.double() + 2 * U * k * x.double().abs(), "dx")
+
+
+def test_training_step_of_a_vanilla_layer():
+    """A whole step of the vanilla layer: router, rows copied to their experts, products, SwiGLU, rows back with the router's
+    weights; every gradient back to the hidden states, the experts' and the router's weights. Against autograd in 64 bits on
+    the same selection; bounds as for the path layer."""
+    T, H, F, n, k = 45, 160, 96, 16, 3
+    g = torch.Generator().manual_seed(8)
+    x, dy = torch.randn((T, H), generator=g), torch.randn((T, H), generator=g)
+    w1, w2 = torch.randn((n, 2 * F, H), generator=g) * 0.08, torch.randn((n, H, F), generator=g) * 0.08
+    wr = torch.randn((n, H), generator=g) * 0.1
+    X, D, W1, W2, WR = (gpu(t) for t in (x, dy, w1, w2, wr))
+    # forward (without paths between experts the path table is the plain dispatch)
+    logits = pcm.pcm_grouped_gemm(X, WR)
+    ids, p, t = pcm.pcm_route_paths(logits, pcm.pcm_mask_pack(torch.eye(n, dtype=torch.uint8, device=DEV)), k)
+    off, of = t.expert_offsets, t.row_of
+    rows = pcm.pcm_dispatch_rows(X, of, offsets=off)
+    gu = pcm.pcm_grouped_gemm(rows, W1, off)
+    u = pcm.pcm_swiglu(gu)
+    o = pcm.pcm_grouped_gemm(u, W2, off)
+    y = pcm.pcm_combine_rows(o, of, p, off)
+    # backward
+    do, dp = pcm.pcm_combine_rows_grad(D, of, o, p, off)
+    du, dW2 = pcm.pcm_grouped_gemm_dx(do, W2, off), pcm.pcm_grouped_gemm_dw(u, do, off)
+    dgu = pcm.pcm_swiglu_grad(gu, du)
+    drows, dW1 = pcm.pcm_grouped_gemm_dx(dgu, W1, off), pcm.pcm_grouped_gemm_dw(rows, dgu, off)
+    dlogits = pcm.pcm_route_grad(ids, p, n, dw=dp)
+    dWR = pcm.pcm_grouped_gemm_dw(X, dlogits)
+    dX = pcm.pcm_dispatch_rows_grad(drows, of, offsets=off)[0] + pcm.pcm_grouped_gemm_dx(dlogits, WR)
+    # 64 bits
+    x64, a64, b64, r64 = (v.double().requires_grad_() for v in (x, w1, w2, wr))
+    sel = ids.cpu().long()
+    p64 = torch.matmul(x64, r64.T).gather(1, sel).softmax(1)
+    v = (a64[sel] @ x64[:, None, :, None])[..., 0]
+    h = torch.nn.functional.silu(v[..., :F]) * v[..., F:]
+    y64 = ((b64[sel] @ h[..., None])[..., 0] * p64[:, :, None]).sum(1)
+    y64.backward(dy.double())
+    for name, got, want in (("y", y, y64.detach()), ("dX", dX, x64.grad), ("dW1", dW1, a64.grad), ("dW2", dW2, b64.grad),
+                            ("dWR", dWR, r64.grad)):
+        rel = float((got.cpu().double() - want).norm() / want.norm())
+        assert rel <= 64 * (2 * F + 8) * 2 * U, (name, rel)
