@@ -432,7 +432,8 @@ pcm_status pcm_combine_rows_grad(pcm_dtype dtype, pcm_dtype o_dtype, pcm_dtype o
                                  void* stream);
 
 /* SwiGLU between the experts' products: u[r, :] = SiLU(gate) * up. gate_up [R, 2F], a row's gate values before its up
- * values; u [R,F]. count: as for pcm_swiglu_quant_fp8, which quantises the same values. */
+ * values; u [R,F]. count: as for pcm_swiglu_quant_fp8, which quantises the same values. SiLU is formed first, in float32:
+ * gates below about -87, where its exponential leaves the normal range, have |gate| 2^-149 |up| of error. */
 pcm_status pcm_swiglu(pcm_dtype dtype, pcm_dtype out_dtype, const void* gate_up, const int32_t* count,
                       int64_t R, int F, void* u, void* stream);
 

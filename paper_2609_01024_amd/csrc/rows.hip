@@ -29,8 +29,8 @@ constexpr int pow2_above(int v) { return v <= 1 ? 1 : 2 * pow2_above((v + 1) / 2
 
 // Sums of N values (a power of two up to 64) over the wavefront, all lanes active: lane l ends with the whole sum of value
 // l * N / 64. While there are several values a step halves them: each lane gives one half away and adds what its partner,
-// on the other side of the step's bit, gives it; then steps of one value. 63 additions for 64 values, where a sum each
-// would take 384. Bits 5 and 4: v_permlane32_swap and 16_swap exchange a half of one register with a half of another;
+// on the other side of the step's bit, gives it; then steps of one value. 32 additions for the 32 values of a mix gradient's
+// wave at eight slots, where a sum each would take 192. Bits 5 and 4: v_permlane32_swap and 16_swap exchange a half of one register with a half of another;
 // below, partners are mirrors in 16 and 8 lanes and neighbours at 2 and 1 (DPP), each of which crosses its bit.
 __device__ __forceinline__ float dpp_f32(float v, const int bit) {
     const int i = __float_as_int(v);
@@ -400,7 +400,10 @@ template <class IN, class OUT, int K, bool STREAM>
 hipError_t mix_sized(bool grad, MixRowsArgs g, hipStream_t s) {
     if (grad && g.dbeta) {
         // A step of 64 C columns a wave (few experts, 7 steps / 1: 131 / 122 us; top-4, F 1408, 3 steps / 1: 107 / 104); where a
-        // wave's sums are many, four (top-8, F 1024, 4 steps / 2 / 1: 82 / 85 / 113). At least four waves a workgroup.
+        // wave's sums are many, four (top-8, F 1024, 4 steps / 2 / 1: 82 / 85 / 113). As many tokens a workgroup as have at
+        // most four waves together, one at least. Above four slots a lane takes four columns of bf16 too: eight do not fit in the
+        // 128 registers of 1024 threads and go to scratch memory (top-8, 8192 tokens, F 1024, 4 columns / 8: 82 / 2665; F 2048
+        // 159 / 3738).
         constexpr int A = K > 4 ? (K + 1) / 2 : K, C = K > 4 ? 4 : kCols<IN, OUT>, kShares = K > 4 ? 2 : 1, kSteps = K > 4 ? 4 : 1;
         constexpr int kMost = kGradThreads / 64 / kShares;
         const int64_t wanted = ceil_div(g.F, 64 * C * kSteps);

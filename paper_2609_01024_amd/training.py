@@ -266,8 +266,8 @@ def pcm_route_grad(topk_ids: torch.Tensor, topk_w: torch.Tensor, n: int, path_bi
 
 # ------------------------------------------------------------------------ all gradients
 def _tensors(tensors: Sequence[torch.Tensor], what: str):
-    """The pcm_tensor array of the tensors (three 64-bit words each), and their counts. (Each attribute of each tensor
-    costs 75 ns: taken by maps, packed by slices.)"""
+    """The pcm_tensor array of the tensors (three 64-bit words each), and their counts. (The five attributes cost 30 to 55 ns
+    each, 0.22 us a tensor: taken by maps, packed by slices.)"""
     T = torch.Tensor
     devices = set(map(T.get_device, tensors))
     if devices and (min(devices) < 0 or devices != {torch.cuda.current_device()} or not all(map(T.is_contiguous, tensors))):
