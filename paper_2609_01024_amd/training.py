@@ -5,9 +5,10 @@ all gradients and clipping.
 As in experts.py the functions carry the C entry points' names, check and marshal their arguments, and allocate what
 the caller does not pass. row_of [T, k] int32, offsets [n+1] int32, path_bits [T] int64 and beta [T, k, k] float32 are
 a PathTable's (or a ScoredPathTable's src_row_of and tgt_row_of). Tensors are float32 or bfloat16, contiguous, on the
-current device and, but for offsets, counts, gradients of the norm and norms, aligned to 16 bytes (a slice of some tokens
-of row_of may not be: it is refused); out_dtype is either type, by default the input's. Sums are float32, rounded once. Autograd does not
-record these calls: a backward pass makes the gradients' calls itself."""
+current device and, but for offsets, counts, norms and the gradients of the norm and the clipping, aligned to 16 bytes (a
+row_of of some tokens, sliced from a larger one, may not be: it is refused); out_dtype is either type, by default the
+input's. Sums are float32, rounded once. Autograd does not record these calls: a backward pass makes the gradients' calls
+itself."""
 from __future__ import annotations
 
 from array import array
